@@ -256,6 +256,137 @@ int32_t vit_forward(spv_ctx* ctx, const spv_vit_config* cfg, const spv_vit_weigh
                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * 8-bit key/value cache (no counterpart in the paper): for a decoder that reads the encoder's
+ * tokens step after step.  Attention of the newest tokens over everything kept, and the paper's
+ * criterion -- rank by the attention received, Sec. 3.3 -- applied to what is kept.
+ *
+ * The cache is a pool of pages.  A page holds `block` tokens of every key head in 8 bits, with
+ * one scale for its keys and one for its values for each head: value = code * scale.  Slot j of a
+ * sequence is row j % block of page page_table[j / block]; slots 0 .. length-1 hold tokens, what
+ * lies behind them is never read as data, whatever bits it has.
+ *
+ * Rules for every entry point of this section
+ *   - lengths and page tables are device arrays.  A page number outside [0, pages), a length
+ *     outside [0, max_length] and a non-finite value handed to kv_cache_append are found on the
+ *     device: the access is skipped (a bad page: its tokens are left out; a bad length: clamped),
+ *     the fault is latched and spv_check() reports SPV_ERR_INVALID_ARG.  The results of such a
+ *     call are undefined, but nothing outside the caller's buffers is touched;
+ *   - the caller sees to it that a page that is written belongs to one sequence; pages that are
+ *     only read may be shared;
+ *   - page_table [batch, columns] has rows `table_stride` entries apart; entries behind a
+ *     sequence's last token are not looked at (kv_cache_evict, kv_cache_read) or may hold anything.
+ * ---------------------------------------------------------------------------------------- */
+enum { SPV_KV_INT8 = 0,  /* codes -127 .. 127                                                   */
+       SPV_KV_E4M3 = 1   /* 8-bit floats, 4 exponent and 3 mantissa bits, largest 448           */ };
+enum { SPV_BF16 = 0, SPV_FP16 = 1, SPV_FP32 = 2 };
+
+typedef struct {
+  int32_t pages, kv_heads, head_dim; /* head_dim 64 or 128                                       */
+  int32_t block;                     /* tokens of a page: 16, 32, 64 or 128                      */
+  int32_t format;                    /* SPV_KV_INT8 | SPV_KV_E4M3                                */
+  void *k, *v;                       /* device, 8-bit codes [pages, kv_heads, block, head_dim]   */
+  float *k_scale, *v_scale;          /* device [pages, kv_heads], positive and finite            */
+} spv_kv_cache;
+
+typedef struct {
+  int32_t batch;
+  int32_t columns;                   /* entries of a row of page_table                           */
+  int64_t table_stride;              /* entries between rows; 0 => columns                       */
+  const int32_t* page_table;         /* device [batch, columns]                                  */
+  const int32_t* lengths;            /* device [batch]: tokens held, see each entry point        */
+  int32_t max_length;                /* no length is larger; 0 => columns * block                */
+} spv_kv_seqs;
+
+/* Append up to `tokens` new tokens to every sequence.  seqs->lengths: tokens held BEFORE the call
+ * (the call does not change it).  counts: device [batch], new tokens of each sequence, 0 .. tokens;
+ * NULL => tokens.  k, v: bf16 or fp16 device tensors addressed as base + b*stride_b +
+ * t*stride_tok + head*stride_head + e (elements; all three multiples of 8).
+ * For each block and head, keys and values apart, with a = largest finite |x| of the new tokens
+ * and M = 127 or 448 the largest code:
+ *   s(a) = the smallest power of two 2^e, e >= -100, with a <= M * 2^e;
+ *   a block that had tokens gets s' = max(its scale, s(a)) and its codes c become
+ *   nearest_even(c * scale / s'); any other gets s' = s(a);  new codes are nearest_even(x / s').
+ * (Powers of two: the quotients are exact, so codes do not depend on the order of arithmetic, a
+ * block that grows token by token is off by less than one step in all, and every value is exact
+ * in bf16.)  Infinities become the largest code of their sign, NaN becomes 0; both are latched.
+ * Asynchronous on `stream`. */
+typedef struct {
+  int32_t tokens;
+  int32_t dtype;                     /* SPV_BF16 | SPV_FP16                                      */
+  int64_t stride_b, stride_tok, stride_head;
+  const int32_t* counts;
+} spv_kv_append_desc;
+int32_t kv_cache_append(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                        const spv_kv_append_desc* desc, const void* k, const void* v, void* stream);
+
+/* Attention of the queries of up to `tokens` tokens of every sequence over its cache.
+ * seqs->lengths: L, tokens held, those of the queries included.  counts: device [batch], n =
+ * queries of each sequence; NULL => tokens.  With query i < n, head h of key head h / (heads /
+ * kv_heads):
+ *   z_j = softmax_scale * <q_i, k_j>,  j < L and, if causal, j <= L - n + i
+ *   o_i = sum_j softmax_j(z) v_j,  lse_i = log sum_j exp z_j
+ * A query without keys gets o = 0 and lse = -inf.  Rows i >= n are not written.
+ * q, o: bf16 or fp16 [batch, tokens, heads, head_dim] with strides (elements, multiples of 8).
+ * lse: optional fp32 [batch, tokens, heads], packed.
+ * weights_out: optional fp32 [batch, kv_heads, >= max_length] with strides:
+ *   weights_out[j] = weights_in[j] + sum of softmax_j over the queries and the heads of a key head,
+ * j < L (weights_in NULL: 0; may be weights_out itself: it then accumulates).  Same strides.
+ * Sums are in fp32 in a fixed order: the same call gives the same bits. */
+typedef struct {
+  int32_t tokens, heads;
+  int32_t dtype;                     /* SPV_BF16 | SPV_FP16                                      */
+  int32_t causal;
+  float softmax_scale;               /* 0 => 1/sqrt(head_dim)                                    */
+  int64_t q_stride_b, q_stride_tok, q_stride_head;
+  int64_t o_stride_b, o_stride_tok, o_stride_head;
+  int64_t w_stride_b, w_stride_head;
+  const int32_t* counts;
+} spv_kv_attn_desc;
+int32_t spv_kv_attention_workspace_size(const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                        const spv_kv_attn_desc* desc, int32_t want_weights, size_t* bytes);
+int32_t kv_cache_attention(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                           const spv_kv_attn_desc* desc, const void* q, void* o, float* lse,
+                           const float* weights_in, float* weights_out, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Keep n = min(L, budget) tokens of every sequence and key head: the first keep_first slots, the
+ * last keep_last, and of the others those of the largest weight (ties to the lower slot, +0 and -0
+ * tie, NaN ranks last).  Survivor t, in ascending slot order, moves to slot t of dst_table's pages
+ * [batch, >= ceil(budget / block)] (rows dst_stride entries apart; none of these pages may be one
+ * that page_table names), or, dst_table NULL, to slot t of the sequence's own pages.  Every
+ * destination block is quantised anew from the survivors' values by kv_cache_append's rule (nothing
+ * is lost where a scale falls).
+ * kept: int32 [batch, kv_heads, budget], old slot of survivor t, -1 behind the last.  weights_out:
+ * optional fp32 [batch, kv_heads, budget] packed, the survivors' weights (what lies behind the last
+ * is left as it was); must not overlap weights_in.  new_lengths: int32 [batch], n; not `lengths`.
+ * weights_in: fp32 [batch, kv_heads, >= max_length] with strides. */
+typedef struct {
+  int32_t budget, keep_first, keep_last; /* keep_first + keep_last <= budget                     */
+  int64_t w_stride_b, w_stride_head;
+  const int32_t* dst_table;
+  int64_t dst_stride;
+} spv_kv_evict_desc;
+int32_t spv_kv_evict_workspace_size(const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                    const spv_kv_evict_desc* desc, size_t* bytes);
+int32_t kv_cache_evict(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                       const spv_kv_evict_desc* desc, const float* weights_in, int32_t* kept,
+                       float* weights_out, int32_t* new_lengths, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* The values of slots first[b] .. first[b] + lengths[b] - 1 of every sequence as dense rows:
+ * k_out, v_out [batch, rows, kv_heads, head_dim] in `dtype`, row i = slot first[b] + i, with
+ * strides (elements; all three multiples of 8).  first NULL => 0.  seqs->lengths: rows wanted,
+ * at most `rows`; rows behind them are left as they were.  Either output may be NULL. */
+typedef struct {
+  int32_t rows;
+  int32_t dtype;                     /* SPV_BF16 | SPV_FP16 | SPV_FP32                           */
+  int64_t stride_b, stride_tok, stride_head;
+  const int32_t* first;
+} spv_kv_read_desc;
+int32_t kv_cache_read(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                      const spv_kv_read_desc* desc, void* k_out, void* v_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Building blocks of vit_forward, exported so that each can be checked and timed alone.
  * ---------------------------------------------------------------------------------------- */
 enum {
@@ -306,7 +437,9 @@ enum {
   SPV_K_FILTER_SELECT = 5, /* head mean + ranking                                              */
   SPV_K_FILTER_GATHER = 6, /* compaction copy of the surviving rows                            */
   SPV_K_MISC = 7,          /* im2col, position tables, output row map                          */
-  SPV_K_COUNT = 8
+  SPV_K_KV_CACHE = 8,      /* kv_cache_append, kv_cache_evict, kv_cache_read                   */
+  SPV_K_KV_ATTN = 9,       /* kv_cache_attention                                               */
+  SPV_K_COUNT = 10
 };
 typedef struct {
   int64_t launches;  /* timed launch groups of this class                                      */

@@ -16,6 +16,8 @@ FILTER_STATIC_BYTES = 2 << 20
 TOKENS_ROW_MAJOR, TOKENS_BLOCK_MAJOR = 0, 1
 MLP_GELU, MLP_SWIGLU = 0, 1
 ATTN_DENSE, ATTN_SPARSE = 0, 1
+KV_INT8, KV_E4M3 = 0, 1
+BF16, FP16, FP32 = 0, 1, 2
 EPI_BIAS, EPI_BIAS_GELU, EPI_BIAS_SILU, EPI_BIAS_MUL, EPI_BIAS_SCALE_RESID, EPI_BIAS_ADDROW = range(6)
 
 EXPORTS = ["spv_create", "spv_destroy", "spv_status_string", "spv_check", "spv_last_wait_site", "spv_launch_count",
@@ -23,6 +25,8 @@ EXPORTS = ["spv_create", "spv_destroy", "spv_status_string", "spv_check", "spv_l
            "spv_filter_keep_count", "spv_filter_workspace_size", "cls_score_topk_filter",
            "cls_score_topk_filter_static",
            "spv_vit_workspace_size", "vit_forward", "spv_gemm_bf16", "spv_layernorm",
+           "kv_cache_append", "spv_kv_attention_workspace_size", "kv_cache_attention",
+           "spv_kv_evict_workspace_size", "kv_cache_evict", "kv_cache_read",
            "spv_profile_enable", "spv_profile_read", "spv_microbench", "spv_selftest_wait"]
 
 
@@ -71,7 +75,7 @@ class VitWeights(C.Structure):
 
 
 KERNEL_CLASSES = ["gemm", "attn_patch", "attn_global", "attn_plan", "layernorm", "filter_select",
-                  "filter_gather", "misc"]
+                  "filter_gather", "misc", "kv_cache", "kv_attn"]
 
 
 class KernelStat(C.Structure):
@@ -84,6 +88,41 @@ class GemmDesc(C.Structure):
                 ("epilogue", C.c_int32), ("bias", C.c_void_p), ("aux", C.c_void_p),
                 ("ldaux", C.c_int64), ("scale", C.c_void_p), ("addrow", C.c_void_p),
                 ("ldadd", C.c_int64), ("rows_per_image", C.c_int32)]
+
+
+class KvCacheStruct(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block", C.c_int32),
+                ("format", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
+class KvSeqs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("columns", C.c_int32), ("table_stride", C.c_int64),
+                ("page_table", C.c_void_p), ("lengths", C.c_void_p), ("max_length", C.c_int32)]
+
+
+class KvAppendDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("dtype", C.c_int32), ("stride_b", C.c_int64), ("stride_tok", C.c_int64),
+                ("stride_head", C.c_int64), ("counts", C.c_void_p)]
+
+
+class KvAttnDesc(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("heads", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32),
+                ("softmax_scale", C.c_float),
+                ("q_stride_b", C.c_int64), ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+                ("o_stride_b", C.c_int64), ("o_stride_tok", C.c_int64), ("o_stride_head", C.c_int64),
+                ("w_stride_b", C.c_int64), ("w_stride_head", C.c_int64), ("counts", C.c_void_p)]
+
+
+class KvEvictDesc(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("keep_first", C.c_int32), ("keep_last", C.c_int32),
+                ("w_stride_b", C.c_int64), ("w_stride_head", C.c_int64), ("dst_table", C.c_void_p),
+                ("dst_stride", C.c_int64)]
+
+
+class KvReadDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("dtype", C.c_int32), ("stride_b", C.c_int64), ("stride_tok", C.c_int64),
+                ("stride_head", C.c_int64), ("first", C.c_void_p)]
 
 
 MICROBENCH_KINDS = {"ex2": 0, "softmax_body": 1, "mma_ss": 2, "mma_ts": 3, "l2_tma": 4}
@@ -137,6 +176,13 @@ def lib():
                                     C.c_void_p]
         L.spv_layernorm.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
                                     C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
+        kv = [C.c_void_p, C.POINTER(KvCacheStruct), C.POINTER(KvSeqs)]
+        L.kv_cache_append.argtypes = kv + [C.POINTER(KvAppendDesc)] + [C.c_void_p] * 3
+        L.spv_kv_attention_workspace_size.argtypes = kv[1:] + [C.POINTER(KvAttnDesc), C.c_int32, C.POINTER(C.c_size_t)]
+        L.kv_cache_attention.argtypes = kv + [C.POINTER(KvAttnDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        L.spv_kv_evict_workspace_size.argtypes = kv[1:] + [C.POINTER(KvEvictDesc), C.POINTER(C.c_size_t)]
+        L.kv_cache_evict.argtypes = kv + [C.POINTER(KvEvictDesc)] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+        L.kv_cache_read.argtypes = kv + [C.POINTER(KvReadDesc)] + [C.c_void_p] * 3
         L.spv_profile_enable.argtypes = [C.c_void_p, C.c_int32]
         L.spv_profile_read.argtypes = [C.c_void_p, C.POINTER(KernelStat)]
         L.spv_selftest_wait.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p]
@@ -163,6 +209,23 @@ def _stream(stream=None):
 def _raise(status, what):
     if status != OK:
         raise SpvError(status, what)
+
+
+def _need(ok, what):
+    """Argument checks of what the library cannot see (types, shapes, devices of the tensors behind the pointers)."""
+    if not ok:
+        raise SpvError(ERR_INVALID_ARG, what)
+
+
+def _apart(t):
+    """Whether an output's strides are those of a view in which the elements do not overlap."""
+    reach = 0
+    for stride, n in sorted(zip(t.stride(), t.shape)):
+        if n > 1:
+            if stride <= reach:
+                return False
+            reach += stride * (n - 1)
+    return True
 
 
 def filter_keep_count(n_patch, keep_ratio):
@@ -210,6 +273,37 @@ def cls_score_topk_filter_static(scores, tokens_in, tokens_out, kept_idx, n_glob
                                                 _stream(stream))
     _raise(st, "cls_score_topk_filter_static")
     return tokens_out, kept_idx
+
+
+class KvCache:
+    """An 8-bit key/value cache: a pool of pages of `block` tokens and one scale for each page and key head
+    (spv_kv_cache in include/spatvit.h).  The tensors are the caller's and are kept alive:
+    k, v int8 or float8_e4m3fn [pages, kv_heads, block, head_dim]; k_scale, v_scale fp32 [pages, kv_heads]."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        fmt = {torch.int8: KV_INT8, torch.float8_e4m3fn: KV_E4M3}.get(k.dtype)
+        _need(fmt is not None and k.dim() == 4 and k.is_contiguous(), "k: contiguous int8 or float8_e4m3fn, 4-D")
+        _need(v.dtype == k.dtype and v.shape == k.shape and v.is_contiguous(), "v: as k")
+        for s in (k_scale, v_scale):
+            _need(s.dtype == torch.float32 and s.shape == k.shape[:2] and s.is_contiguous(),
+                  "scales: contiguous fp32 [pages, kv_heads]")
+        _need(k.is_cuda and all(t.device == k.device for t in (v, k_scale, v_scale)), "one CUDA device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self.pages, self.kv_heads, self.block, self.head_dim = k.shape
+        self.struct = KvCacheStruct(self.pages, self.kv_heads, self.head_dim, self.block, fmt, k.data_ptr(),
+                                    v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, pages, kv_heads, head_dim, block=64, format=KV_INT8, device="cuda"):
+        """A pool of its own; nothing in it is defined until it is appended."""
+        import torch
+        dt = {KV_INT8: torch.int8, KV_E4M3: torch.float8_e4m3fn}[format]
+        shape = (pages, kv_heads, block, head_dim)
+        return cls(torch.empty(shape, dtype=dt, device=device), torch.empty(shape, dtype=dt, device=device),
+                   torch.empty(shape[:2], dtype=torch.float32, device=device),
+                   torch.empty(shape[:2], dtype=torch.float32, device=device))
 
 
 class Context:
@@ -332,6 +426,173 @@ class Context:
                                            _ptr(sc), _ptr(workspace), workspace.numel(), _stream(stream))
         _raise(st, "spatial_block_attention")
         return out, sc
+
+    # -- 8-bit key/value cache ------------------------------------------------------------------
+    def _kv_seqs(self, cache, page_table, lengths, max_length=0):
+        torch = self._torch
+        _need(cache.device == self.device == page_table.device == lengths.device, "cache, tables: the context's device")
+        B, cols = page_table.shape
+        _need(page_table.dtype == torch.int32 and page_table.stride(1) == 1 and (B == 1 or page_table.stride(0) >= cols),
+              "page_table: int32 [batch, columns], rows apart")
+        _need(lengths.dtype == torch.int32 and lengths.shape == (B,) and lengths.is_contiguous(), "lengths: int32 [batch]")
+        return KvSeqs(B, cols, page_table.stride(0) if B > 1 else 0, page_table.data_ptr(), lengths.data_ptr(), max_length)
+
+    def _kv_vector(self, t, B, what):
+        if t is None:
+            return None
+        _need(t.dtype == self._torch.int32 and t.shape == (B,) and t.is_contiguous() and t.device == self.device,
+              what + ": int32 [batch]")
+        return t.data_ptr()
+
+    def _kv_scratch(self, nbytes, workspace, stream):
+        """The caller's workspace, or one from torch's allocator in the order of the call's stream: a captured
+        graph then owns its own, and calls on two streams do not share one."""
+        if workspace is not None or nbytes == 0:
+            return workspace
+        if stream is None:
+            return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+        with self._torch.cuda.stream(stream):
+            return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+
+    def _kv_dtype(self, t):
+        torch = self._torch
+        dt = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(t.dtype)
+        _need(dt is not None and t.dim() == 4 and t.stride(3) == 1 and t.device == self.device,
+              "bf16, fp16 (or, of kv_cache_read, fp32) [batch, tokens, heads, head_dim], head_dim contiguous, on the "
+              "context's device")
+        return dt
+
+    def _kv_weights(self, cache, w, B):
+        _need(w.dtype == self._torch.float32 and w.dim() == 3 and w.shape[:2] == (B, cache.kv_heads) and
+              w.stride(2) == 1 and w.device == self.device, "weights: fp32 [batch, kv_heads, slots], slots contiguous")
+
+    def kv_cache_append(self, cache, k, v, page_table, lengths, counts=None, stream=None):
+        """Quantise new tokens' keys and values into the cache, behind the `lengths` that each sequence holds.
+        k, v: bf16 or fp16 [B, tokens, kv_heads, head_dim] views with the same strides; counts: int32 [B], new
+        tokens of each sequence (default: all).  `lengths` is not changed: add the counts to it afterwards."""
+        dt = self._kv_dtype(k)
+        B, n, h, d = k.shape
+        _need(v.dtype == k.dtype and v.shape == k.shape and v.stride() == k.stride() and v.device == k.device, "v: as k")
+        _need(h == cache.kv_heads and d == cache.head_dim and page_table.shape[0] == B, "k: the cache's heads and head_dim")
+        seqs = self._kv_seqs(cache, page_table, lengths)
+        sb, st, sh, _ = k.stride()
+        desc = KvAppendDesc(n, dt, sb, st, sh, self._kv_vector(counts, B, "counts"))
+        _raise(lib().kv_cache_append(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(k), _ptr(v),
+                                     _stream(stream)), "kv_cache_append")
+
+    def kv_cache_attention(self, cache, q, page_table, lengths, counts=None, causal=True, scale=0.0, out=None, lse=None,
+                           weights_in=None, weights_out=None, max_length=None, workspace=None, stream=None):
+        """Attention of q (bf16 or fp16 [B, tokens, heads, head_dim] view) over the cache; `lengths` include the
+        queries' own tokens.  counts: int32 [B], queries of each sequence (default: all; rows behind them are not
+        written).  lse: optional fp32 [B, tokens, heads] to fill.  weights_out: optional fp32 [B, kv_heads, slots]:
+        weights_in (default 0; may be weights_out itself) plus the attention weight that every kept token received.
+        max_length: no sequence is longer (default: what the table and the weights have room for).  Returns out."""
+        torch = self._torch
+        dt = self._kv_dtype(q)
+        B, n, H, d = q.shape
+        _need(d == cache.head_dim and page_table.shape[0] == B, "q: [batch, tokens, heads, the cache's head_dim]")
+        if out is None:
+            out = torch.empty((B, n, H, d), dtype=q.dtype, device=q.device)
+        _need(out.dtype == q.dtype and out.shape == q.shape and out.stride(3) == 1 and out.device == q.device and
+              _apart(out), "out: as q, no two elements at one place")
+        limit = page_table.shape[1] * cache.block
+        wb = wh = 0
+        if weights_out is not None:
+            self._kv_weights(cache, weights_out, B)
+            _need(_apart(weights_out), "weights_out: no two elements at one place")
+            limit = min(limit, weights_out.shape[2])
+            wb, wh, _ = weights_out.stride()
+            if weights_in is not None and weights_in is not weights_out:
+                self._kv_weights(cache, weights_in, B)
+                _need(weights_in.shape == weights_out.shape and weights_in.stride() == weights_out.stride(),
+                      "weights_in: as weights_out")
+        if max_length is not None:
+            _need(1 <= max_length <= limit, "max_length: 1 .. what the table and the weights have room for")
+            limit = max_length
+        if lse is not None:
+            _need(lse.dtype == torch.float32 and lse.shape == (B, n, H) and lse.is_contiguous() and lse.device == q.device,
+                  "lse: fp32 [batch, tokens, heads]")
+        seqs = self._kv_seqs(cache, page_table, lengths, limit)
+        desc = KvAttnDesc(n, H, dt, int(causal), float(scale), *q.stride()[:3], *out.stride()[:3], wb, wh,
+                          self._kv_vector(counts, B, "counts"))
+        need = C.c_size_t(0)
+        _raise(lib().spv_kv_attention_workspace_size(C.byref(cache.struct), C.byref(seqs), C.byref(desc),
+                                                     weights_out is not None, C.byref(need)),
+               "spv_kv_attention_workspace_size")
+        ws = self._kv_scratch(need.value, workspace, stream)
+        _raise(lib().kv_cache_attention(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(q),
+                                        _ptr(out), _ptr(lse), _ptr(weights_in), _ptr(weights_out), _ptr(ws),
+                                        0 if ws is None else ws.numel(), _stream(stream)), "kv_cache_attention")
+        return out
+
+    def kv_cache_evict(self, cache, weights, page_table, lengths, budget, keep_first=0, keep_last=0, dst_table=None,
+                       kept=None, weights_out=None, new_lengths=None, max_length=None, workspace=None, stream=None):
+        """Keep min(length, budget) tokens of every sequence and key head: the first keep_first, the last keep_last
+        and of the others those of the largest weight (fp32 [B, kv_heads, slots]); moved together, in order, onto
+        dst_table's pages (int32 [B, columns]; none of them a page of page_table), or, without one, onto the
+        sequence's own.  Returns (kept int32 [B, kv_heads, budget], new_lengths int32 [B], weights_out fp32
+        [B, kv_heads, budget])."""
+        torch = self._torch
+        self._kv_weights(cache, weights, page_table.shape[0])
+        B, h = page_table.shape[0], cache.kv_heads
+        limit = min(page_table.shape[1] * cache.block, weights.shape[2])
+        if max_length is not None:
+            _need(1 <= max_length <= limit, "max_length: 1 .. what the table and the weights have room for")
+            limit = max_length
+        seqs = self._kv_seqs(cache, page_table, lengths, limit)
+        _need(int(budget) >= 1, "budget: 1 or more")
+        if kept is None:
+            kept = torch.empty((B, h, budget), dtype=torch.int32, device=self.device)
+        if weights_out is None:
+            weights_out = torch.zeros((B, h, budget), dtype=torch.float32, device=self.device)
+        if new_lengths is None:
+            new_lengths = torch.empty((B,), dtype=torch.int32, device=self.device)
+        _need(kept.dtype == torch.int32 and kept.shape == (B, h, budget) and kept.is_contiguous() and
+              kept.device == self.device, "kept: int32 [batch, kv_heads, budget]")
+        _need(weights_out.dtype == torch.float32 and weights_out.shape == kept.shape and weights_out.is_contiguous() and
+              weights_out.device == self.device, "weights_out: fp32 [batch, kv_heads, budget]")
+        nl = self._kv_vector(new_lengths, B, "new_lengths")
+        dst, stride = None, 0
+        if dst_table is not None:
+            _need(dst_table.dtype == torch.int32 and dst_table.dim() == 2 and dst_table.shape[0] == B and
+                  dst_table.stride(1) == 1 and dst_table.shape[1] * cache.block >= budget and
+                  (B == 1 or dst_table.stride(0) >= dst_table.shape[1]) and dst_table.device == self.device, "dst_table: int32 [batch, budget / block or more]")
+            dst, stride = dst_table.data_ptr(), dst_table.stride(0) if B > 1 else 0
+        desc = KvEvictDesc(budget, keep_first, keep_last, weights.stride(0), weights.stride(1), dst, stride)
+        need = C.c_size_t(0)
+        _raise(lib().spv_kv_evict_workspace_size(C.byref(cache.struct), C.byref(seqs), C.byref(desc), C.byref(need)),
+               "spv_kv_evict_workspace_size")
+        ws = self._kv_scratch(need.value, workspace, stream)
+        _raise(lib().kv_cache_evict(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(weights),
+                                    _ptr(kept), _ptr(weights_out), nl, _ptr(ws), 0 if ws is None else ws.numel(),
+                                    _stream(stream)), "kv_cache_evict")
+        return kept, new_lengths, weights_out
+
+    def kv_cache_read(self, cache, page_table, counts, first=None, k_out=None, v_out=None, rows=None, dtype=None,
+                      stream=None):
+        """The values of slots first[b] (default 0) .. first[b] + counts[b] - 1 as rows 0 .. of k_out, v_out
+        [B, rows, kv_heads, head_dim] (bf16, fp16 or fp32 views with the same strides; rows behind counts[b] are left
+        as they were).  Without outputs, zeroed ones of `rows` rows and `dtype` (default bf16) are made; a single
+        output may be given for only that half.  Returns (k_out, v_out)."""
+        torch = self._torch
+        B = page_table.shape[0]
+        if k_out is None and v_out is None:
+            rows = page_table.shape[1] * cache.block if rows is None else rows
+            shape = (B, rows, cache.kv_heads, cache.head_dim)
+            k_out = torch.zeros(shape, dtype=dtype or torch.bfloat16, device=self.device)
+            v_out = torch.zeros_like(k_out)
+        o = k_out if k_out is not None else v_out
+        dt = self._kv_dtype(o)
+        _need(_apart(o) and o.shape[0] == B and o.shape[2:] == (cache.kv_heads, cache.head_dim), "outputs: [batch, rows, kv_heads, head_dim]")
+        if k_out is not None and v_out is not None:
+            _need(v_out.dtype == o.dtype and v_out.shape == o.shape and v_out.stride() == o.stride() and
+                  v_out.device == o.device, "v_out: as k_out")
+        seqs = self._kv_seqs(cache, page_table, counts)
+        sb, st, sh, _ = o.stride()
+        desc = KvReadDesc(o.shape[1], dt, sb, st, sh, self._kv_vector(first, B, "first"))
+        _raise(lib().kv_cache_read(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(k_out),
+                                   _ptr(v_out), _stream(stream)), "kv_cache_read")
+        return k_out, v_out
 
     # -- building blocks ----------------------------------------------------------------------
     def gemm_bf16(self, a, w, out, epilogue=EPI_BIAS, bias=None, aux=None, scale=None, addrow=None,

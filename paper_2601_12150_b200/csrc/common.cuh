@@ -43,7 +43,8 @@ void spv_prof_end(spv_ctx* ctx, int32_t token, cudaStream_t stream, double work)
 #include <nvtx3/nvToolsExt.h>
 static inline void spv_nvtx_push(int32_t cls) {
   static const char* const names[SPV_K_COUNT] = {"spv:gemm", "spv:attn_patch", "spv:attn_global", "spv:attn_plan",
-                                                 "spv:layernorm", "spv:filter_select", "spv:filter_gather", "spv:misc"};
+                                                 "spv:layernorm", "spv:filter_select", "spv:filter_gather", "spv:misc",
+                                                 "spv:kv_cache", "spv:kv_attn"};
   nvtxRangePushA(cls >= 0 && cls < SPV_K_COUNT ? names[cls] : "spv");
 }
 static inline void spv_nvtx_pop() { nvtxRangePop(); }
@@ -63,6 +64,9 @@ struct SpvProfScope {
 // these as SPV_ERR_INVALID_ARG.
 #define SPV_SITE_BAD_KEPT_INDEX 0xB001u   // forced_keep of vit_forward
 #define SPV_SITE_BAD_PATCH_POS 0xB002u    // patch_pos of spatial_block_attention
+#define SPV_SITE_KV_PAGE 0xB003u          // page number of a kv_cache_* call
+#define SPV_SITE_KV_LENGTH 0xB004u        // length, count or first slot of a kv_cache_* call
+#define SPV_SITE_KV_VALUE 0xB005u         // non-finite value handed to kv_cache_append
 
 #define SPV_CUDA_OK(expr)                         \
   do {                                            \

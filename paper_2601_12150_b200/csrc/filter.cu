@@ -10,19 +10,14 @@
 //                     ordered two-counter scan that emits the kept indices in ascending order;
 //   filter_gather     128-bit row copy of the global tokens and the kept rows.
 #include "filter.cuh"
+#include "select.cuh"
 
 namespace {
 
-constexpr int kSelThreads = 1024;
+using spv::block_scan2;
+using spv::kSelThreads;
+using spv::rank_key;
 constexpr int kSelItems = 4;
-
-// Larger mean -> larger key.  +0 and -0 share a key; NaN gets key 0 (ranks last).
-__device__ __forceinline__ uint32_t rank_key(float m) {
-  if (m != m) return 0u;
-  if (m == 0.0f) m = 0.0f;   // folds -0 into +0
-  uint32_t u = __float_as_uint(m);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
 
 __global__ void __launch_bounds__(256) filter_mean_key(const float* __restrict__ scores, int heads, int n_patch,
                                                        int npad, float* __restrict__ mean_ws,
@@ -68,38 +63,6 @@ __global__ void __launch_bounds__(256) filter_mean_key_logits(const float* __res
   const int pos = cur_pos ? __ldg(cur_pos + (size_t)b * n_cur + t) : t;
   mean_ws[(size_t)b * npad + pos] = mean;
   key_ws[(size_t)b * npad + pos] = rank_key(mean);
-}
-
-// Block-wide exclusive scan of two counters; returns this thread's exclusive prefixes and the
-// block totals.  Called by all kSelThreads threads.
-__device__ __forceinline__ void block_scan2(int a, int b, int& ea, int& eb, int& ta, int& tb, int (*warp_tot)[2]) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int ia = a, ib = b;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    int na = __shfl_up_sync(0xffffffffu, ia, o), nb = __shfl_up_sync(0xffffffffu, ib, o);
-    if (lane >= o) { ia += na; ib += nb; }
-  }
-  if (lane == 31) { warp_tot[warp][0] = ia; warp_tot[warp][1] = ib; }
-  __syncthreads();
-  if (warp == 0) {
-    int wa = warp_tot[lane][0], wb = warp_tot[lane][1];
-    int sa = wa, sb = wb;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      int na = __shfl_up_sync(0xffffffffu, sa, o), nb = __shfl_up_sync(0xffffffffu, sb, o);
-      if (lane >= o) { sa += na; sb += nb; }
-    }
-    warp_tot[lane][0] = sa - wa;   // exclusive warp offsets
-    warp_tot[lane][1] = sb - wb;
-    if (lane == 31) { warp_tot[32][0] = sa; warp_tot[32][1] = sb; }
-  }
-  __syncthreads();
-  ea = warp_tot[warp][0] + ia - a;
-  eb = warp_tot[warp][1] + ib - b;
-  ta = warp_tot[32][0];
-  tb = warp_tot[32][1];
-  __syncthreads();
 }
 
 __global__ void __launch_bounds__(kSelThreads) filter_select(const uint32_t* __restrict__ key_ws, int n_patch,

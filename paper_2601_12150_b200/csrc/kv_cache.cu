@@ -1,0 +1,575 @@
+// 8-bit key/value cache: append, eviction by accumulated attention weight, read-back.
+//
+//   kv_append_kernel   one CTA per touched (page, head, keys | values): the new rows stay in registers between
+//                      the largest-magnitude reduction and the conversion, so each crosses HBM once;
+//   kv_select_kernel   one CTA per (sequence, head): radix select of the survivors, ascending slots;
+//   kv_gather_kernel   one CTA per destination (page, head, keys | values): gathers the survivors' codes, which
+//                      stay in registers while the block's new scale is found;
+//   kv_place_kernel    eviction in place only: staged pages back over the sequence's own;
+//   kv_read_kernel     codes to 16- or 32-bit rows.
+#include "kv_cache.cuh"
+#include "select.cuh"
+
+#include <type_traits>
+
+namespace {
+
+using namespace spv;
+
+constexpr int kThreads = 256;
+
+// Largest of the threads' values, in every thread.
+__device__ __forceinline__ uint32_t block_max(uint32_t x, uint32_t* warp_max) {
+  x = __reduce_max_sync(0xffffffffu, x);
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = x;
+  __syncthreads();
+  uint32_t m = warp_max[0];
+#pragma unroll
+  for (int i = 1; i < kThreads / 32; ++i) m = max(m, warp_max[i]);
+  return m;
+}
+
+struct AppendArgs {
+  const uint16_t* src[2];
+  int64_t stride_b, stride_tok, stride_head;
+  const int32_t* counts;
+  int32_t tokens, block;
+};
+
+template <int FMT, int DT, int D>
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, AppendArgs a) {
+  constexpr int kVecRow = D / 8;                          // 16-byte vectors of a new row
+  constexpr int kMaxVec = 128 * kVecRow / kThreads;       // of a whole block, per thread
+  __shared__ uint32_t warp_max[kThreads / 32];
+  const int b = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+  const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
+  int cnt = a.counts ? kv_clamped(__ldg(a.counts + b), a.tokens, c.status) : a.tokens;
+  cnt = kv_clamped(cnt, c.max_length - len, c.status);
+  const SpvKvSpan span = spv_kv_append_span(len, cnt, a.block, blockIdx.x);
+  const int lo = span.lo, hi = span.hi;
+  if (lo >= hi) return;
+  const int page = kv_page(c.table + b * c.table_stride, span.column, c.pages, c.status);
+  if (page < 0) return;
+  const uint16_t* src = a.src[which] + b * a.stride_b + (int64_t)(lo - len) * a.stride_tok + head * a.stride_head;
+  const int nvec = (hi - lo) * kVecRow;
+  uint4 x[kMaxVec];
+  uint32_t big = 0;
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    const int v = threadIdx.x + i * kThreads;
+    if (v < nvec) x[i] = __ldg(reinterpret_cast<const uint4*>(src + (v / kVecRow) * a.stride_tok) + v % kVecRow);
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    if (threadIdx.x + i * kThreads < nvec) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 f = kv_unpack2<DT>(w[j]);
+        const uint32_t p = __float_as_uint(f.x) & 0x7FFFFFFFu, q = __float_as_uint(f.y) & 0x7FFFFFFFu;
+        odd |= p >= 0x7F800000u || q >= 0x7F800000u;
+        big = max(big, max(p < 0x7F800000u ? p : 0u, q < 0x7F800000u ? q : 0u));
+      }
+    }
+  }
+  if (odd) kv_fault(c.status, SPV_SITE_KV_VALUE);
+  big = block_max(big, warp_max);
+  float* scale_at = const_cast<float*>(which ? c.v_scale : c.k_scale) + (size_t)page * c.kv_heads + head;
+  uint8_t* codes = const_cast<uint8_t*>(which ? c.v : c.k) + ((size_t)page * c.kv_heads + head) * a.block * D;
+  float scale = kv_pow2(kv_exponent<FMT>(big));
+  const int held = lo - span.base;                        // rows that were there before the call
+  if (held > 0) {
+    const float old = *scale_at;
+    if (!(scale > old)) {
+      scale = old;
+    } else {
+      const float f = old / scale;
+      for (int v = threadIdx.x; v < held * (D / 16); v += kThreads) {
+        uint4* at = reinterpret_cast<uint4*>(codes) + v;
+        uint4 t = *at;
+        uint32_t* w = &t.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float y[4];
+          kv_decode4<FMT>(w[j], y);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] *= f;
+          w[j] = kv_encode4<FMT>(y);
+        }
+        *at = t;
+      }
+    }
+  }
+  const float inv = 1.0f / scale;
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    const int v = threadIdx.x + i * kThreads;
+    if (v < nvec) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      uint32_t out[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float2 p = kv_unpack2<DT>(w[2 * j]), q = kv_unpack2<DT>(w[2 * j + 1]);
+        const float y[4] = {p.x * inv, p.y * inv, q.x * inv, q.y * inv};
+        out[j] = kv_encode4<FMT>(y);
+      }
+      *reinterpret_cast<uint2*>(codes + (size_t)(held + v / kVecRow) * D + (v % kVecRow) * 8) = make_uint2(out[0], out[1]);
+    }
+  }
+  __syncthreads();                                        // every thread has read the old scale
+  if (threadIdx.x == 0) *scale_at = scale;
+}
+
+struct ReadArgs {
+  void* out[2];
+  int64_t stride_b, stride_tok, stride_head;
+  const int32_t* first;
+  int32_t rows, block;
+};
+
+template <int FMT, int DT, int D>
+__global__ void __launch_bounds__(kThreads) kv_read_kernel(KvView c, ReadArgs a) {
+  constexpr int kVecRow = D / 16;                         // 16 codes a thread
+  constexpr int kRowsPass = kThreads / kVecRow;
+  constexpr int kPasses = 64 / kRowsPass;                 // 64 rows a CTA
+  const int b = blockIdx.z, head = blockIdx.y;
+  const int n = min(kv_clamped(__ldg(c.lengths + b), a.rows, c.status), a.rows);
+  const int first = a.first ? kv_clamped(__ldg(a.first + b), c.max_length, c.status) : 0;
+  const int end = kv_clamped(first + n, c.max_length, c.status);
+  const int32_t* row = c.table + b * c.table_stride;
+  const int col = (threadIdx.x % kVecRow) * 16;
+  uint4 x[kPasses][2];
+  float s[kPasses][2];
+  int at[kPasses];
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int r = blockIdx.x * 64 + i * kRowsPass + threadIdx.x / kVecRow;
+    const int slot = first + r;
+    at[i] = -1;
+    if (slot < end) {
+      const int page = kv_page(row, slot / a.block, c.pages, c.status);
+      if (page >= 0) {
+        at[i] = r;
+        const size_t ph = (size_t)page * c.kv_heads + head;
+        const size_t o = (size_t)spv_kv_row(page, c.kv_heads, head, a.block, slot) * D + col;
+        if (a.out[0]) { x[i][0] = __ldcs(reinterpret_cast<const uint4*>(c.k + o)); s[i][0] = __ldg(c.k_scale + ph); }
+        if (a.out[1]) { x[i][1] = __ldcs(reinterpret_cast<const uint4*>(c.v + o)); s[i][1] = __ldg(c.v_scale + ph); }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    if (at[i] < 0) continue;
+    const int64_t o = b * a.stride_b + (int64_t)at[i] * a.stride_tok + head * a.stride_head + col;
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      if (!a.out[m]) continue;
+      const uint32_t w[4] = {x[i][m].x, x[i][m].y, x[i][m].z, x[i][m].w};
+      float y[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        kv_decode4<FMT>(w[j], y + 4 * j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[4 * j + e] *= s[i][m];
+      }
+      if constexpr (DT == SPV_FP32) {
+        float4* dst = reinterpret_cast<float4*>((float*)a.out[m] + o);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) __stcs(dst + j, make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]));
+      } else {
+        uint4* dst = reinterpret_cast<uint4*>((uint16_t*)a.out[m] + o);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float* z = y + 8 * j;
+          __stcs(dst + j, make_uint4(kv_pack2<DT>(z[0], z[1]), kv_pack2<DT>(z[2], z[3]), kv_pack2<DT>(z[4], z[5]),
+                                     kv_pack2<DT>(z[6], z[7])));
+        }
+      }
+    }
+  }
+}
+
+struct EvictArgs {
+  const float* weights;
+  int64_t w_stride_b, w_stride_head;
+  int32_t budget, keep_first, keep_last, block;
+  int32_t* kept;
+  float* weights_out;
+  int32_t* new_lengths;
+  const int32_t* dst_table;     // NULL: page b * dst_blocks + column of the destination pool
+  int64_t dst_stride;
+  int32_t dst_blocks, dst_pages;
+  uint8_t* dst_k;
+  uint8_t* dst_v;
+  float* dst_ks;
+  float* dst_vs;
+};
+
+__global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictArgs a) {
+  __shared__ int hist[256];
+  __shared__ int warp_tot[33][2];
+  __shared__ uint32_t s_prefix;
+  __shared__ int s_remaining;
+  const int head = blockIdx.x, b = blockIdx.y;
+  const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
+  const int n = min(len, a.budget);
+  int32_t* kout = a.kept + ((size_t)b * c.kv_heads + head) * a.budget;
+  for (int t = n + threadIdx.x; t < a.budget; t += kSelThreads) kout[t] = -1;
+  if (head == 0 && threadIdx.x == 0) a.new_lengths[b] = n;
+  if (n == len) {
+    for (int t = threadIdx.x; t < n; t += kSelThreads) kout[t] = t;
+    return;
+  }
+  // the protected ends, then the k largest of the slots between them
+  for (int t = threadIdx.x; t < a.keep_first; t += kSelThreads) kout[t] = t;
+  for (int t = threadIdx.x; t < a.keep_last; t += kSelThreads) kout[n - a.keep_last + t] = len - a.keep_last + t;
+  const int k = n - a.keep_first - a.keep_last;
+  const int m = len - a.keep_first - a.keep_last;
+  if (k == 0) return;
+  const float* w = a.weights + b * a.w_stride_b + head * a.w_stride_head + a.keep_first;
+  kout += a.keep_first;
+  if (threadIdx.x == 0) { s_prefix = 0u; s_remaining = k; }
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
+    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+    __syncthreads();
+    const uint32_t prefix = s_prefix;
+    const uint32_t himask = pass == 0 ? 0u : (0xFFFFFFFFu << (shift + 8));
+    for (int i = threadIdx.x; i < m; i += kSelThreads) {
+      const uint32_t e = rank_key(__ldg(w + i));
+      if ((e & himask) == prefix) atomicAdd(&hist[(e >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int rem = s_remaining, bin = 255;
+      for (; bin > 0; --bin) {
+        if (hist[bin] >= rem) break;
+        rem -= hist[bin];
+      }
+      s_prefix = prefix | ((uint32_t)bin << shift);
+      s_remaining = rem;
+    }
+    __syncthreads();
+  }
+  const uint32_t thr = s_prefix;     // k-th largest key
+  const int need_eq = s_remaining;   // how many keys equal to it stay (lowest slots first)
+  int base_gt = 0, base_eq = 0;
+  for (int tile0 = 0; tile0 < m; tile0 += 4 * kSelThreads) {
+    const int j0 = tile0 + 4 * threadIdx.x;
+    uint32_t e[4];
+    int gt = 0, eq = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool valid = j0 + t < m;
+      e[t] = valid ? rank_key(__ldg(w + j0 + t)) : 0u;
+      gt += valid && e[t] > thr ? 1 : 0;
+      eq += valid && e[t] == thr ? 1 : 0;
+    }
+    int egt, eeq, tgt, teq;
+    block_scan2(gt, eq, egt, eeq, tgt, teq, warp_tot);
+    int pgt = base_gt + egt, peq = base_eq + eeq;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool valid = j0 + t < m, is_gt = valid && e[t] > thr, is_eq = valid && e[t] == thr;
+      if (is_gt || (is_eq && peq < need_eq)) kout[pgt + min(peq, need_eq)] = a.keep_first + j0 + t;
+      pgt += is_gt ? 1 : 0;
+      peq += is_eq ? 1 : 0;
+    }
+    base_gt += tgt;
+    base_eq += teq;
+  }
+}
+
+template <int FMT, int D>
+__global__ void __launch_bounds__(kThreads) kv_gather_kernel(KvView c, EvictArgs a) {
+  constexpr int kVecRow = D / 16;
+  constexpr int kMaxVec = 128 * kVecRow / kThreads;
+  __shared__ uint32_t warp_max[kThreads / 32];
+  const int b = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, column = blockIdx.x;
+  const int len = min(max(__ldg(c.lengths + b), 0), c.max_length);
+  const int n = min(len, a.budget);
+  const int base = column * a.block, rows = min(a.block, n - base);
+  if (rows <= 0) return;
+  const int32_t* kept = a.kept + ((size_t)b * c.kv_heads + head) * a.budget + base;
+  const int32_t* row = c.table + b * c.table_stride;
+  const uint8_t* src = which ? c.v : c.k;
+  const float* src_scale = which ? c.v_scale : c.k_scale;
+  if (which == 0 && a.weights_out) {
+    const float* w = a.weights + b * a.w_stride_b + head * a.w_stride_head;
+    float* out = a.weights_out + ((size_t)b * c.kv_heads + head) * a.budget + base;
+    for (int t = threadIdx.x; t < rows; t += kThreads) out[t] = __ldg(w + kept[t]);
+  }
+  const int nvec = rows * kVecRow;
+  uint4 x[kMaxVec];
+  float s[kMaxVec];
+  uint32_t big = 0;
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    const int v = threadIdx.x + i * kThreads;
+    x[i] = make_uint4(0u, 0u, 0u, 0u);
+    s[i] = 0.0f;
+    if (v < nvec) {
+      const int slot = kept[v / kVecRow];
+      const int page = kv_page(row, slot / a.block, c.pages, c.status);
+      if (page >= 0) {
+        const size_t ph = (size_t)page * c.kv_heads + head;
+        x[i] = __ldcs(reinterpret_cast<const uint4*>(src + spv_kv_row(page, c.kv_heads, head, a.block, slot) * D) + v % kVecRow);
+        s[i] = __ldg(src_scale + ph);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float y[4];
+      kv_decode4<FMT>(w[j], y);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t u = __float_as_uint(y[e] * s[i]) & 0x7FFFFFFFu;
+        big = max(big, u < 0x7F800000u ? u : 0u);
+      }
+    }
+  }
+  big = block_max(big, warp_max);
+  const int page = a.dst_table ? kv_page(a.dst_table + b * a.dst_stride, column, a.dst_pages, c.status)
+                               : b * a.dst_blocks + column;
+  if (page < 0) return;
+  const float scale = kv_pow2(kv_exponent<FMT>(big)), inv = 1.0f / scale;
+  const size_t ph = (size_t)page * c.kv_heads + head;
+  uint4* dst = reinterpret_cast<uint4*>((which ? a.dst_v : a.dst_k) + ph * a.block * D);
+#pragma unroll
+  for (int i = 0; i < kMaxVec; ++i) {
+    const int v = threadIdx.x + i * kThreads;
+    if (v < nvec) {
+      uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float y[4];
+        kv_decode4<FMT>(w[j], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = y[e] * s[i] * inv;
+        w[j] = kv_encode4<FMT>(y);
+      }
+      dst[v] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  if (threadIdx.x == 0) (which ? a.dst_vs : a.dst_ks)[ph] = scale;
+}
+
+// Staged page b * dst_blocks + column over page `column` of sequence b: the rows that hold survivors, and the scale.
+__global__ void __launch_bounds__(kThreads) kv_place_kernel(KvView c, EvictArgs a, int row_vec) {
+  const int b = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, column = blockIdx.x;
+  const int n = min(min(max(__ldg(c.lengths + b), 0), c.max_length), a.budget);
+  const int rows = min(a.block, n - column * a.block);
+  if (rows <= 0) return;
+  const int page = kv_page(c.table + b * c.table_stride, column, c.pages, c.status);
+  if (page < 0) return;
+  const size_t from = (size_t)(b * a.dst_blocks + column) * c.kv_heads + head, to = (size_t)page * c.kv_heads + head;
+  const uint4* src = reinterpret_cast<const uint4*>(which ? a.dst_v : a.dst_k) + from * a.block * row_vec;
+  uint4* dst = reinterpret_cast<uint4*>(const_cast<uint8_t*>(which ? c.v : c.k)) + to * a.block * row_vec;
+  for (int v = threadIdx.x; v < rows * row_vec; v += kThreads) dst[v] = src[v];
+  if (threadIdx.x == 0) const_cast<float*>(which ? c.v_scale : c.k_scale)[to] = (which ? a.dst_vs : a.dst_ks)[from];
+}
+
+// ---- host ------------------------------------------------------------------------------------
+// Calls f with the format and the head size as compile-time constants.
+template <typename F>
+void by_format(const spv_kv_cache* c, F f) {
+  if (c->format == SPV_KV_INT8) {
+    if (c->head_dim == 64) f(std::integral_constant<int, SPV_KV_INT8>(), std::integral_constant<int, 64>());
+    else f(std::integral_constant<int, SPV_KV_INT8>(), std::integral_constant<int, 128>());
+  } else {
+    if (c->head_dim == 64) f(std::integral_constant<int, SPV_KV_E4M3>(), std::integral_constant<int, 64>());
+    else f(std::integral_constant<int, SPV_KV_E4M3>(), std::integral_constant<int, 128>());
+  }
+}
+
+inline bool unaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+
+struct StagePlan { size_t codes, scales, total; };
+StagePlan stage_plan(const spv_kv_cache* c, const spv_kv_seqs* s, const spv_kv_evict_desc* d) {
+  const size_t pages = (size_t)s->batch * ((d->budget + c->block - 1) / c->block);
+  StagePlan p;
+  p.codes = spv_align_up(pages * c->kv_heads * c->block * c->head_dim, 256);
+  p.scales = spv_align_up(pages * c->kv_heads * sizeof(float), 256);
+  p.total = 2 * (p.codes + p.scales);
+  return p;
+}
+
+int32_t check_evict(const spv_kv_cache* c, const spv_kv_seqs* s, const spv_kv_evict_desc* d) {
+  int32_t st = spv_kv_check_cache(c);
+  if (st != SPV_OK) return st;
+  if ((st = spv_kv_check_seqs(c, s)) != SPV_OK) return st;
+  if (!d || d->budget < 1 || d->keep_first < 0 || d->keep_last < 0) return SPV_ERR_INVALID_ARG;
+  if ((int64_t)d->keep_first + d->keep_last > d->budget) return SPV_ERR_INVALID_ARG;
+  const int64_t blocks = ((int64_t)d->budget + c->block - 1) / c->block;
+  if (d->budget > (int64_t)s->columns * c->block && !d->dst_table) return SPV_ERR_INVALID_ARG;
+  if (blocks * s->batch > INT32_MAX) return SPV_ERR_UNSUPPORTED;
+  if (d->dst_table) {
+    if (d->dst_table == s->page_table || d->dst_stride < 0) return SPV_ERR_INVALID_ARG;
+    if (d->dst_stride && d->dst_stride < blocks) return SPV_ERR_INVALID_ARG;
+  }
+  if (d->w_stride_b < 0 || d->w_stride_head < 0) return SPV_ERR_INVALID_ARG;
+  return SPV_OK;
+}
+
+}  // namespace
+
+int32_t spv_kv_check_cache(const spv_kv_cache* c) {
+  if (!c || c->pages < 1 || c->kv_heads < 1) return SPV_ERR_INVALID_ARG;
+  if (c->format != SPV_KV_INT8 && c->format != SPV_KV_E4M3) return SPV_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return SPV_ERR_UNSUPPORTED;
+  if (c->block != 16 && c->block != 32 && c->block != 64 && c->block != 128) return SPV_ERR_UNSUPPORTED;
+  if (c->kv_heads > 4096) return SPV_ERR_UNSUPPORTED;
+  // rows of the pool are numbered in 31 bits
+  if ((int64_t)c->pages * c->kv_heads * c->block > INT32_MAX) return SPV_ERR_UNSUPPORTED;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale) return SPV_ERR_INVALID_ARG;
+  if (unaligned(c->k) || unaligned(c->v) || ((uintptr_t)c->k_scale & 3u) || ((uintptr_t)c->v_scale & 3u))
+    return SPV_ERR_ALIGNMENT;
+  return SPV_OK;
+}
+
+int32_t spv_kv_check_seqs(const spv_kv_cache* c, const spv_kv_seqs* s) {
+  if (!s || s->batch < 1 || s->columns < 1 || !s->page_table || !s->lengths) return SPV_ERR_INVALID_ARG;
+  if (s->batch > 65535) return SPV_ERR_UNSUPPORTED;
+  const int64_t cap = (int64_t)s->columns * c->block;
+  if (cap > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
+  if (s->max_length < 0 || s->max_length > cap) return SPV_ERR_INVALID_ARG;
+  if (s->table_stride < 0 || (s->table_stride && s->table_stride < s->columns)) return SPV_ERR_INVALID_ARG;
+  if (((uintptr_t)s->page_table & 3u) || ((uintptr_t)s->lengths & 3u)) return SPV_ERR_ALIGNMENT;
+  return SPV_OK;
+}
+
+extern "C" int32_t kv_cache_append(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                   const spv_kv_append_desc* d, const void* k, const void* v, void* stream_) {
+  int32_t st = spv_kv_check_cache(cache);
+  if (st != SPV_OK) return st;
+  if ((st = spv_kv_check_seqs(cache, seqs)) != SPV_OK) return st;
+  if (!d || d->tokens < 1 || !k || !v) return SPV_ERR_INVALID_ARG;
+  if (d->dtype != SPV_BF16 && d->dtype != SPV_FP16) return SPV_ERR_UNSUPPORTED;
+  if (unaligned(k) || unaligned(v) || d->stride_b % 8 || d->stride_tok % 8 || d->stride_head % 8) return SPV_ERR_ALIGNMENT;
+  if (!ctx || spv_on_device(ctx) != SPV_OK) return SPV_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  const KvView view = kv_view(ctx, cache, seqs);
+  AppendArgs a;
+  a.src[0] = (const uint16_t*)k;
+  a.src[1] = (const uint16_t*)v;
+  a.stride_b = d->stride_b;
+  a.stride_tok = d->stride_tok;
+  a.stride_head = d->stride_head;
+  a.counts = d->counts;
+  a.tokens = d->tokens;
+  a.block = cache->block;
+  // blocks that `tokens` new rows can touch, wherever in a block they begin
+  const int64_t most = ((int64_t)d->tokens + cache->block - 2) / cache->block + 1;
+  const unsigned nb = (unsigned)(most < seqs->columns ? most : seqs->columns);
+  const dim3 grid(nb, 2 * cache->kv_heads, seqs->batch);
+  SpvProfScope prof(ctx, SPV_K_KV_CACHE, stream);
+  by_format(cache, [&](auto fmt, auto dim) {
+    if (d->dtype == SPV_BF16) kv_append_kernel<fmt(), SPV_BF16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+    else kv_append_kernel<fmt(), SPV_FP16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+  });
+  return spv_launch_ok(ctx);
+}
+
+extern "C" int32_t kv_cache_read(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                 const spv_kv_read_desc* d, void* k_out, void* v_out, void* stream_) {
+  int32_t st = spv_kv_check_cache(cache);
+  if (st != SPV_OK) return st;
+  if ((st = spv_kv_check_seqs(cache, seqs)) != SPV_OK) return st;
+  if (!d || d->rows < 1 || (!k_out && !v_out)) return SPV_ERR_INVALID_ARG;
+  if (d->dtype != SPV_BF16 && d->dtype != SPV_FP16 && d->dtype != SPV_FP32) return SPV_ERR_UNSUPPORTED;
+  if (unaligned(k_out) || unaligned(v_out) || d->stride_b % 8 || d->stride_tok % 8 || d->stride_head % 8)
+    return SPV_ERR_ALIGNMENT;
+  if (!ctx || spv_on_device(ctx) != SPV_OK) return SPV_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  const KvView view = kv_view(ctx, cache, seqs);
+  ReadArgs a;
+  a.out[0] = k_out;
+  a.out[1] = v_out;
+  a.stride_b = d->stride_b;
+  a.stride_tok = d->stride_tok;
+  a.stride_head = d->stride_head;
+  a.first = d->first;
+  a.rows = d->rows;
+  a.block = cache->block;
+  const dim3 grid((d->rows + 63) / 64, cache->kv_heads, seqs->batch);
+  SpvProfScope prof(ctx, SPV_K_KV_CACHE, stream);
+  by_format(cache, [&](auto fmt, auto dim) {
+    if (d->dtype == SPV_BF16) kv_read_kernel<fmt(), SPV_BF16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+    else if (d->dtype == SPV_FP16) kv_read_kernel<fmt(), SPV_FP16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+    else kv_read_kernel<fmt(), SPV_FP32, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+  });
+  return spv_launch_ok(ctx);
+}
+
+extern "C" int32_t spv_kv_evict_workspace_size(const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                               const spv_kv_evict_desc* d, size_t* bytes) {
+  const int32_t st = check_evict(cache, seqs, d);
+  if (st != SPV_OK) return st;
+  if (!bytes) return SPV_ERR_INVALID_ARG;
+  *bytes = d->dst_table ? 0 : stage_plan(cache, seqs, d).total;
+  return SPV_OK;
+}
+
+extern "C" int32_t kv_cache_evict(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs,
+                                  const spv_kv_evict_desc* d, const float* weights_in, int32_t* kept, float* weights_out,
+                                  int32_t* new_lengths, void* workspace, size_t workspace_bytes, void* stream_) {
+  const int32_t st = check_evict(cache, seqs, d);
+  if (st != SPV_OK) return st;
+  if (!weights_in || !kept || !new_lengths || new_lengths == seqs->lengths) return SPV_ERR_INVALID_ARG;
+  if (((uintptr_t)weights_in & 3u) || ((uintptr_t)kept & 3u) || ((uintptr_t)weights_out & 3u) ||
+      ((uintptr_t)new_lengths & 3u))
+    return SPV_ERR_ALIGNMENT;
+  const int32_t max_length = spv_kv_max_length(cache, seqs);
+  if (weights_out) {   // packed output against the span of the strided input
+    const float* in_end = weights_in + (seqs->batch - 1) * d->w_stride_b + (cache->kv_heads - 1) * d->w_stride_head + max_length;
+    const float* out_end = weights_out + (size_t)seqs->batch * cache->kv_heads * d->budget;
+    if (weights_out < in_end && weights_in < out_end) return SPV_ERR_INVALID_ARG;
+  }
+  if (!ctx || spv_on_device(ctx) != SPV_OK) return SPV_ERR_INVALID_ARG;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  const KvView view = kv_view(ctx, cache, seqs);
+  EvictArgs a;
+  a.weights = weights_in;
+  a.w_stride_b = d->w_stride_b;
+  a.w_stride_head = d->w_stride_head;
+  a.budget = d->budget;
+  a.keep_first = d->keep_first;
+  a.keep_last = d->keep_last;
+  a.block = cache->block;
+  a.kept = kept;
+  a.weights_out = weights_out;
+  a.new_lengths = new_lengths;
+  a.dst_blocks = (d->budget + cache->block - 1) / cache->block;
+  a.dst_table = d->dst_table;
+  a.dst_stride = d->dst_stride ? d->dst_stride : a.dst_blocks;
+  a.dst_pages = cache->pages;
+  if (d->dst_table) {
+    a.dst_k = (uint8_t*)cache->k;
+    a.dst_v = (uint8_t*)cache->v;
+    a.dst_ks = cache->k_scale;
+    a.dst_vs = cache->v_scale;
+  } else {
+    const StagePlan p = stage_plan(cache, seqs, d);
+    if (!workspace || workspace_bytes < p.total || ((uintptr_t)workspace & 255u)) return SPV_ERR_WORKSPACE;
+    a.dst_k = (uint8_t*)workspace;
+    a.dst_v = a.dst_k + p.codes;
+    a.dst_ks = (float*)(a.dst_v + p.codes);
+    a.dst_vs = (float*)((char*)a.dst_ks + p.scales);
+  }
+  const dim3 grid(a.dst_blocks, 2 * cache->kv_heads, seqs->batch);
+  SpvProfScope prof(ctx, SPV_K_KV_CACHE, stream);
+  kv_select_kernel<<<dim3(cache->kv_heads, seqs->batch), kSelThreads, 0, stream>>>(view, a);
+  by_format(cache, [&](auto fmt, auto dim) {
+    kv_gather_kernel<fmt(), dim()><<<grid, kThreads, 0, stream>>>(view, a);
+  });
+  if (!d->dst_table) {
+    kv_place_kernel<<<grid, kThreads, 0, stream>>>(view, a, cache->head_dim / 16);
+    return spv_launch_ok(ctx, 3);
+  }
+  return spv_launch_ok(ctx, 2);
+}

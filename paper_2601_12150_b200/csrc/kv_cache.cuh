@@ -1,0 +1,122 @@
+// Shared parts of the 8-bit key/value cache kernels: argument checks, scales and codes, slot -> page.
+#pragma once
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "kv_index.cuh"
+
+// ---- host: checks that need no device ------------------------------------------------------
+int32_t spv_kv_check_cache(const spv_kv_cache* c);
+int32_t spv_kv_check_seqs(const spv_kv_cache* c, const spv_kv_seqs* s);
+static inline int32_t spv_kv_max_length(const spv_kv_cache* c, const spv_kv_seqs* s) {
+  const int64_t cap = (int64_t)s->columns * c->block;
+  return s->max_length > 0 ? s->max_length : (int32_t)cap;
+}
+static inline int64_t spv_kv_table_stride(const spv_kv_seqs* s) { return s->table_stride ? s->table_stride : s->columns; }
+
+#ifdef __CUDACC__
+namespace spv {
+
+// What every kernel of the section gets: the pool and the sequences.
+struct KvView {
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* table;
+  const int32_t* lengths;
+  uint32_t* status;        // status word 1 of the context: first fault found in the caller's arrays
+  int64_t table_stride;
+  int32_t pages, kv_heads, max_length;
+};
+
+static inline KvView kv_view(const spv_ctx* ctx, const spv_kv_cache* c, const spv_kv_seqs* s) {
+  KvView w;
+  w.k = (const uint8_t*)c->k;
+  w.v = (const uint8_t*)c->v;
+  w.k_scale = c->k_scale;
+  w.v_scale = c->v_scale;
+  w.table = s->page_table;
+  w.lengths = s->lengths;
+  w.status = ctx->d_status + 1;
+  w.table_stride = spv_kv_table_stride(s);
+  w.pages = c->pages;
+  w.kv_heads = c->kv_heads;
+  w.max_length = spv_kv_max_length(c, s);
+  return w;
+}
+
+__device__ __forceinline__ void kv_fault(uint32_t* status, uint32_t site) { atomicCAS(status, 0u, site); }
+
+// A number of the caller's clamped to [0, most]; a number outside is latched.
+__device__ __forceinline__ int kv_clamped(int x, int most, uint32_t* status) {
+  const int y = spv_kv_clamp(x, most);
+  if (y != x) kv_fault(status, SPV_SITE_KV_LENGTH);
+  return y;
+}
+
+// A page number, or -1 (and the fault latched) where it is none of the pool's.
+__device__ __forceinline__ int kv_page(const int32_t* table_row, int column, int pages, uint32_t* status) {
+  const int p = __ldg(table_row + column);
+  if (spv_kv_valid_page(p, pages)) return p;
+  kv_fault(status, SPV_SITE_KV_PAGE);
+  return -1;
+}
+
+// ---- scales: the smallest power of two s = 2^e, e >= -100, with a <= M s.  `a` by its fp32 bits, finite.
+// 127 = 1.984375 * 2^6 and 448 = 1.75 * 2^8, so the exponent is a's own, less 6 or 8, and one more where a's
+// significand is above that of M: no rounding anywhere.
+template <int FMT>
+__device__ __forceinline__ int kv_exponent(uint32_t a) {
+  constexpr uint32_t kEdge = FMT == SPV_KV_INT8 ? 0x7E0000u : 0x600000u;
+  constexpr int kTop = FMT == SPV_KV_INT8 ? 6 : 8;
+  const int e = (int)(a >> 23) - 127 - kTop + ((a & 0x7FFFFFu) > kEdge ? 1 : 0);
+  return max(e, -100);
+}
+__device__ __forceinline__ float kv_pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+
+// ---- codes ---------------------------------------------------------------------------------
+// Nearest code of x (already divided by its scale), ties to even; beyond the largest code the largest; NaN is 0.
+template <int FMT>
+__device__ __forceinline__ uint32_t kv_code(float x) {
+  if (x != x) x = 0.0f;
+  if (FMT == SPV_KV_INT8) return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.0f), 127.0f)) & 0xFFu;
+  return (uint32_t)__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+}
+// The four codes of a 32-bit word as fp32.
+template <int FMT>
+__device__ __forceinline__ void kv_decode4(uint32_t w, float* x) {
+  if (FMT == SPV_KV_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int)(int8_t)(w >> (8 * i));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * i)), __NV_E4M3);
+      const float2 f = __half22float2(__half2(h));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t kv_encode4(const float* x) {
+  return kv_code<FMT>(x[0]) | kv_code<FMT>(x[1]) << 8 | kv_code<FMT>(x[2]) << 16 | kv_code<FMT>(x[3]) << 24;
+}
+
+// two 16-bit values <-> fp32
+template <int DT>
+__device__ __forceinline__ float2 kv_unpack2(uint32_t u) {
+  if (DT == SPV_BF16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+template <int DT>
+__device__ __forceinline__ uint32_t kv_pack2(float lo, float hi) {
+  if (DT == SPV_BF16) return pack_bf16(lo, hi);
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+}  // namespace spv
+#endif

@@ -1,0 +1,37 @@
+// Index arithmetic of the 8-bit cache that depends on numbers read from the caller's device arrays (lengths,
+// counts, page numbers): plain C++, so that it can be run on the host with numbers that no caller should pass.
+#pragma once
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define SPV_HD __host__ __device__ __forceinline__
+#else
+#define SPV_HD static inline
+#endif
+
+SPV_HD int spv_kv_clamp(int x, int most) { return x < 0 ? 0 : (x > most ? most : x); }
+SPV_HD bool spv_kv_valid_page(int page, int pages) { return (uint32_t)page < (uint32_t)pages; }
+
+// Row of the pool (head_dim codes each) that holds `slot` of a sequence and head on a valid page.
+SPV_HD int64_t spv_kv_row(int page, int kv_heads, int head, int block, int slot) {
+  return ((int64_t)page * kv_heads + head) * block + slot % block;
+}
+
+// Slots [lo, hi) that the append writes on the page `column`, the `touched`-th that new tokens can reach; lo >= hi:
+// none.  len and cnt are already within [0, max_length] and [0, max_length - len].
+struct SpvKvSpan { int column, base, lo, hi; };
+SPV_HD SpvKvSpan spv_kv_append_span(int len, int cnt, int block, int touched) {
+  SpvKvSpan s;
+  s.column = len / block + touched;
+  s.base = s.column * block;
+  s.lo = len > s.base ? len : s.base;
+  s.hi = len + cnt < s.base + block ? len + cnt : s.base + block;
+  return s;
+}
+
+// Keys that query i of n sees: slots [0, end).
+SPV_HD int spv_kv_query_end(int len, int n, int i, int causal) {
+  if (!causal) return len;
+  const int64_t end = (int64_t)len - n + i + 1;
+  return end < 0 ? 0 : (end > len ? len : (int)end);
+}

@@ -1,0 +1,657 @@
+"""GPU parity of the 8-bit key/value cache operators against their definitions in 64 bits.
+
+Codes, scales, kept slots and read-back values are compared for equality: a power-of-two scale makes every quotient
+exact, so there is one right code.  Attention is compared element by element with a bound derived from its arithmetic
+(see bounds())."""
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+FORMATS, TYPES = ["int8", "e4m3"], ["bf16", "fp16"]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    import paper_2601_12150_b200 as spv
+    c = spv.Context(0)
+    yield c
+    c.close()
+
+
+def make_cache(ctx, pages, heads, dim, block, fmt, garbage=True):
+    """A pool whose every code and scale is something no kernel may use: NaN codes (e4m3), huge and NaN scales."""
+    import paper_2601_12150_b200 as spv
+    cache = spv.KvCache.empty(pages, heads, dim, block, spv.KV_INT8 if fmt == "int8" else spv.KV_E4M3, ctx.device)
+    for t in (cache.k, cache.v):
+        t.view(torch.int8).fill_(-127 if fmt == "int8" else 127)      # 0x7F: e4m3's NaN
+    for t in (cache.k_scale, cache.v_scale):
+        t.fill_(float("nan") if garbage else 1.0)
+    return cache
+
+
+def make_table(rng, needs, block, pages, columns, device):
+    """Shuffled pages; entries behind a sequence's last page are numbers that name no page."""
+    order = rng.permutation(pages)
+    table = np.full((len(needs), columns), 1 << 30, dtype=np.int32)
+    table[:, 1::2] = -7
+    at = 0
+    for b, n in enumerate(needs):
+        used = (n + block - 1) // block
+        table[b, :used] = order[at:at + used]
+        at += used
+    assert at <= pages
+    return table, torch.from_numpy(table).to(device)
+
+
+def normals(rng, shape, dtype, spread=1.0):
+    x = rng.standard_normal(shape) * np.exp(0.5 * rng.standard_normal(shape[:-2] + (1, 1))) * spread
+    return torch.from_numpy(x.astype(np.float32)).to(ref.TORCH_TYPE[dtype])
+
+
+def filled(ctx, rng, lengths, heads, dim, block, fmt, dtype, room=0, extra_pages=2, strided=True):
+    """A cache that holds `lengths` tokens appended by the library, and the CPU pool that follows it."""
+    needs = [n + room for n in lengths]
+    pages = sum((n + block - 1) // block for n in needs) + extra_pages
+    columns = max(1, max((n + block - 1) // block for n in needs)) + 1
+    cache = make_cache(ctx, pages, heads, dim, block, fmt)
+    table, dtable = make_table(rng, needs, block, pages, columns, ctx.device)
+    most = max(1, max(lengths))
+    k, v = normals(rng, (len(lengths), most, heads, dim), dtype), normals(rng, (len(lengths), most, heads, dim), dtype, 0.7)
+    pool = ref.Pool(pages, heads, block, dim, fmt)
+    zero = torch.zeros(len(lengths), dtype=torch.int32, device=ctx.device)
+    counts = torch.tensor(lengths, dtype=torch.int32, device=ctx.device)
+    kd, vd = as_views(ctx, k, v) if strided else (k.to(ctx.device), v.to(ctx.device))
+    ctx.kv_cache_append(cache, kd, vd, dtable, zero, counts=counts)
+    ctx.check()
+    for b, n in enumerate(lengths):
+        for h in range(heads):
+            pool.append("k", table[b], 0, k[b, :n, h].double().numpy(), h)
+            pool.append("v", table[b], 0, v[b, :n, h].double().numpy(), h)
+    return cache, pool, table, dtable, counts
+
+
+def as_views(ctx, *xs):
+    """Side by side in one buffer, as a projection leaves them."""
+    fused = torch.cat(xs, dim=2).to(ctx.device)
+    out, at = [], 0
+    for x in xs:
+        out.append(fused[:, :, at:at + x.shape[2]])
+        at += x.shape[2]
+    return out
+
+
+def same_state(cache, pool, table, lengths):
+    """Codes of all held slots and the scales of their pages, bit for bit."""
+    got = ref.Pool.of(cache)
+    for b, n in enumerate(lengths):
+        for m in "kv":
+            for h in range(cache.kv_heads):
+                used = (n + cache.block - 1) // cache.block
+                pg = table[b, :used]
+                assert np.array_equal(got.scale[m][pg, h], pool.scale[m][pg, h]), (b, m, h)
+                slots = np.arange(n)
+                at = (table[b][slots // cache.block], h, slots % cache.block)
+                assert np.array_equal(got.codes[m][at], pool.codes[m][at]), (b, m, h)
+
+
+# ---- append ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("block,dim,heads", [(16, 64, 3), (32, 128, 2), (64, 64, 1), (128, 128, 2)])
+def test_append_whole_and_token_by_token(ctx, fmt, dtype, block, dim, heads):
+    rng = np.random.default_rng(block + dim)
+    lengths = [0, 1, block - 1, block, block + 1, 3 * block + 5]
+    cache, pool, table, dtable, dlen = filled(ctx, rng, lengths, heads, dim, block, fmt, dtype, room=block + 9)
+    same_state(cache, pool, table, lengths)
+    lens = list(lengths)
+    for step, n in enumerate([1, 1, 3, block]):     # scales grow: the later tokens are larger
+        k = normals(rng, (len(lens), n, heads, dim), dtype, 2.0 ** step)
+        v = normals(rng, (len(lens), n, heads, dim), dtype, 0.1)
+        counts = [n if (b + step) % 3 else n // 2 for b in range(len(lens))]
+        kd, vd = as_views(ctx, k, v)
+        ctx.kv_cache_append(cache, kd, vd, dtable, dlen,
+                            counts=torch.tensor(counts, dtype=torch.int32, device=ctx.device))
+        ctx.check()
+        for b, c in enumerate(counts):
+            for h in range(heads):
+                pool.append("k", table[b], lens[b], k[b, :c, h].double().numpy(), h)
+                pool.append("v", table[b], lens[b], v[b, :c, h].double().numpy(), h)
+        lens = [a + c for a, c in zip(lens, counts)]
+        dlen = torch.tensor(lens, dtype=torch.int32, device=ctx.device)
+        same_state(cache, pool, table, lens)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_edges_of_the_scale(ctx, fmt):
+    """Largest magnitudes at, below and above M * 2^e; zeros; the smallest and the largest finite values."""
+    m = ref.M[fmt]
+    tops = [m, m * 0.5, np.nextafter(np.float32(m), 0), m * 2 ** 20, 1.0, 255.0, 256.0, 0.0, 2.0 ** -126, 3e38, 1e-30]
+    heads, dim, block = len(tops), 64, 16
+    k = torch.zeros((1, 5, heads, dim), dtype=torch.float32)
+    for h, t in enumerate(tops):
+        k[0, 2, h, 7] = float(t)
+        k[0, 3, h, :] = -float(t) * torch.linspace(0, 1, dim)
+    k = k.to(torch.bfloat16)
+    cache = make_cache(ctx, 2, heads, dim, block, fmt)
+    table = torch.tensor([[1]], dtype=torch.int32, device=ctx.device)
+    zero = torch.zeros(1, dtype=torch.int32, device=ctx.device)
+    kd = k.to(ctx.device)
+    ctx.kv_cache_append(cache, kd, kd.clone(), table, zero)
+    ctx.check()
+    pool = ref.Pool(2, heads, block, dim, fmt)
+    for h in range(heads):
+        for which in "kv":
+            pool.append(which, [1], 0, k[0, :, h].double().numpy(), h)
+    same_state(cache, pool, np.array([[1]]), [5])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_append_non_finite_values_are_latched(ctx, fmt):
+    import paper_2601_12150_b200 as spv
+    cache = make_cache(ctx, 1, 1, 64, 16, fmt)
+    k = torch.ones((1, 4, 1, 64), dtype=torch.bfloat16)
+    k[0, 1, 0, 3], k[0, 2, 0, 4], k[0, 3, 0, 5] = float("inf"), -float("inf"), float("nan")
+    table = torch.zeros((1, 1), dtype=torch.int32, device=ctx.device)
+    zero = torch.zeros(1, dtype=torch.int32, device=ctx.device)
+    ctx.kv_cache_append(cache, k.to(ctx.device), k.to(ctx.device), table, zero)
+    with pytest.raises(spv.SpvError) as e:
+        ctx.check()
+    assert e.value.status == spv.ERR_INVALID_ARG
+    ctx.check()                                      # cleared
+    got = ref.Pool.of(cache)
+    row = got.codes["k"][0, 0]
+    one = 1.0 / ref.scale_of(1.0, fmt)
+    assert row[1, 3] == ref.M[fmt] and row[2, 4] == -ref.M[fmt] and row[3, 5] == 0.0 and row[0, 0] == one
+
+
+# ---- read --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("out_type", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("block,dim", [(16, 128), (64, 64), (128, 64)])
+def test_read(ctx, fmt, out_type, block, dim):
+    rng = np.random.default_rng(3)
+    lengths, heads = [0, 1, 2 * block + 3, 131], 3
+    cache, pool, table, dtable, dlen = filled(ctx, rng, lengths, heads, dim, block, fmt, "bf16")
+    first = [0, 0, 5, 64]
+    counts = [0, 1, 2 * block - 2, 60]
+    rows = max(counts) + 2
+    fused = torch.full((len(lengths), rows, 2 * heads, dim), 7.0, dtype=out_type, device=ctx.device)
+    ko, vo = fused[:, :, :heads], fused[:, :, heads:]
+    ctx.kv_cache_read(cache, dtable, torch.tensor(counts, dtype=torch.int32, device=ctx.device),
+                      first=torch.tensor(first, dtype=torch.int32, device=ctx.device), k_out=ko, v_out=vo)
+    ctx.check()
+    for b, (f, n) in enumerate(zip(first, counts)):
+        for m, o in (("k", ko), ("v", vo)):
+            assert torch.all(o[b, n:] == 7.0)
+            for h in range(heads):
+                want = pool.rows(m, table[b], np.arange(f, f + n), h)
+                want = torch.from_numpy(want).to(torch.float32).to(out_type)   # exact in bf16 and fp32
+                assert torch.equal(o[b, :n, h].cpu(), want)
+    only_v = torch.zeros((len(lengths), rows, heads, dim), dtype=out_type, device=ctx.device)
+    assert ctx.kv_cache_read(cache, dtable, dlen.clamp(max=rows), v_out=only_v)[0] is None
+    ctx.check()
+    for b, n in enumerate(lengths):
+        n = min(n, rows)
+        assert torch.all(only_v[b, n:] == 0)
+        for h in range(heads):
+            want = torch.from_numpy(pool.rows("v", table[b], np.arange(n), h)).to(torch.float32).to(out_type)
+            assert torch.equal(only_v[b, :n, h].cpu(), want)
+
+
+# ---- attention ---------------------------------------------------------------------------------
+def bounds(o, spread, reach, vmax, dim, length, dtype):
+    """|computed - exact| at most, element by element.
+    Logits: products of a query and a code are exact in fp32; their sum of `dim` terms is off by at most
+    dim * 2^-23 * sum|q k| (tensor-core sums may truncate: 2^-23, not 2^-24), the scale and the shift by the maximum
+    add three roundings of values up to 2 reach.  dz = (dim + 6) * 2^-23 * reach.
+    Probabilities: exp2 within 2^-21, so p is off by (2 dz + 2^-20) of itself, numerator and sum together; a
+    probability may be held in 16 bits (11 significant) for the product with the values: 2^-11 of itself, or, where
+    it is below 2^-14 of the largest, 2^-25 of the largest, for each key.
+    The sum over the keys in fp32: length * 2^-23 of sum p |v| at most, and far less in blocks: 64 terms at a time,
+    the blocks' sums one after the other: (64 + length / 64) * 2^-23.
+    The result is rounded to its type: eps / 2 of it (and half the smallest subnormal)."""
+    dz = (dim + 6) * 2.0 ** -23 * reach
+    rel = 2 * dz + 2.0 ** -20 + 2.0 ** -11 + (64 + length / 64) * 2.0 ** -23
+    eps = torch.finfo(ref.TORCH_TYPE[dtype]).eps
+    tiny = torch.finfo(ref.TORCH_TYPE[dtype]).smallest_normal * eps
+    return rel[..., None] * spread * (1 + eps) + length * 2.0 ** -25 * vmax[..., None] + eps / 2 * np.abs(o) + tiny
+
+
+def run_attention(ctx, rng, lengths, tokens, counts, heads, kv_heads, dim, block, fmt, dtype, causal, weights=True,
+                  scale=0.0, qscale=1.5, state=None):
+    B = len(lengths)
+    cache, pool, table, dtable, dlen = state or filled(ctx, rng, lengths, kv_heads, dim, block, fmt, dtype)
+    q = normals(rng, (B, tokens, heads, dim), dtype, qscale)
+    other = normals(rng, (B, tokens, 2, dim), dtype)
+    qd, _ = as_views(ctx, q, other)
+    out = torch.full((B, tokens, heads + 1, dim), 7.0, dtype=q.dtype, device=ctx.device)
+    lse = torch.full((B, tokens, heads), 7.0, device=ctx.device)
+    width = max(1, max(lengths)) + 3
+    w_in = torch.from_numpy(rng.random((B, kv_heads, width)).astype(np.float32)).to(ctx.device)
+    w_out = torch.full((B, kv_heads, width), 7.0, device=ctx.device)
+    dcounts = None if counts is None else torch.tensor(counts, dtype=torch.int32, device=ctx.device)
+    args = dict(counts=dcounts, causal=causal, scale=scale, out=out[:, :, :heads])
+    if weights:
+        args.update(weights_in=w_in, weights_out=w_out)
+    ctx.kv_cache_attention(cache, qd, dtable, dlen, lse=lse, **args)
+    ctx.check()
+    assert torch.all(out[:, :, heads] == 7.0)
+    got, glse, gw = out.cpu().double().numpy(), lse.cpu().double().numpy(), w_out.cpu().double().numpy()
+    win = w_in.cpu().double().numpy()
+    sc = scale or dim ** -0.5
+    for b, length in enumerate(lengths):
+        n = tokens if counts is None else counts[b]
+        o, l, w, spread, reach, vmax = ref.attention(pool, table[b], q[b].double().numpy(), length, n, heads, kv_heads,
+                                                     causal, sc)
+        lim = bounds(o, spread, reach, vmax, dim, max(length, 1), dtype)
+        err = np.abs(got[b, :n, :heads] - o)
+        assert np.all(err <= lim), (b, length, n, float((err / lim).max()))
+        assert np.all(got[b, n:, :heads] == 7.0) and np.all(glse[b, n:] == 7.0)
+        some = np.isfinite(l)
+        assert np.array_equal(np.isfinite(glse[b, :n]), some) and np.all(glse[b, :n][~some] == -np.inf)
+        dz = (dim + 6) * 2.0 ** -23 * reach
+        lim = 2 * dz + 2.0 ** -20 + (64 + length / 64) * 2.0 ** -23 + 2.0 ** -22 * np.abs(np.where(some, l, 0.0))
+        assert np.all(np.abs(np.where(some, glse[b, :n] - np.where(some, l, 0.0), 0.0)) <= lim)
+        if weights:
+            # every probability from its logit and the log-sum, both off by dz; then sums of n * group terms in fp32
+            worst = float(reach.max()) if reach.size else 0.0
+            rel = 3 * (dim + 6) * 2.0 ** -23 * worst + 2.0 ** -19 + (64 + length / 64 + n * heads // kv_heads) * 2.0 ** -23
+            rel += 2.0 ** -22 * float(np.abs(l[some]).max()) if some.any() else 0.0
+            want = win[b, :, :length] + w
+            assert np.all(np.abs(gw[b, :, :length] - want) <= rel * w + 2.0 ** -24 * np.abs(want) + 1e-37), (b, length)
+            assert np.all(gw[b, :, length:] == 7.0)
+    return out, lse, w_out
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("block,dim,kv_heads,group", [(16, 64, 4, 1), (32, 128, 2, 4), (64, 128, 1, 8), (128, 64, 3, 5),
+                                                      (64, 64, 2, 16), (16, 128, 1, 24)])
+def test_attention_single_token(ctx, fmt, dtype, block, dim, kv_heads, group):
+    rng = np.random.default_rng(block * dim + group)
+    lengths = [1, 0, 15, 16, 17, 63, 64, 65, 127, 128, 129, 700]
+    run_attention(ctx, rng, lengths, 1, None, kv_heads * group, kv_heads, dim, block, fmt, dtype, True)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("int8", "bf16"), ("e4m3", "fp16")])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("tokens,group,block,dim", [(2, 1, 16, 64), (5, 3, 64, 128), (9, 1, 32, 64), (16, 2, 128, 128),
+                                                    (33, 4, 64, 64), (130, 1, 16, 128), (257, 2, 64, 64)])
+def test_attention_several_tokens(ctx, fmt, dtype, causal, tokens, group, block, dim):
+    """Padded batches; sequences with fewer keys than queries (causal rows without a key), and with none."""
+    rng = np.random.default_rng(tokens + group)
+    lengths = [tokens, 0, 1, tokens + 1, 300 + tokens, max(1, tokens - 3), 64]
+    counts = [tokens, tokens, min(tokens, 3), 0, tokens, tokens, tokens // 2]
+    run_attention(ctx, rng, lengths, tokens, counts, 2 * group, 2, dim, block, fmt, dtype, causal)
+
+
+@pytest.mark.parametrize("fmt,dtype,dim", [("int8", "fp16", 128), ("e4m3", "bf16", 64)])
+def test_attention_long(ctx, fmt, dtype, dim):
+    rng = np.random.default_rng(5)
+    run_attention(ctx, rng, [20011, 3, 777], 1, None, 8, 2, dim, 64, fmt, dtype, True)
+    run_attention(ctx, rng, [5003], 4, None, 12, 1, dim, 128, fmt, dtype, True, weights=False)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_uneven_scales(ctx, fmt):
+    """Blocks whose keys and values differ by many powers of two, an all-zero block, one far larger than the rest."""
+    rng = np.random.default_rng(8)
+    block, dim, heads = 16, 64, 1
+    n = 10 * block
+    k, v = normals(rng, (1, n, heads, dim), "bf16", 0.3), normals(rng, (1, n, heads, dim), "bf16")
+    for i, e in enumerate([0, 12, -30, 0, 40, -60, 3, 0, -8, 20]):
+        v[0, i * block:(i + 1) * block] = v[0, i * block:(i + 1) * block] * 2.0 ** e
+        if i % 3:
+            k[0, i * block:(i + 1) * block] = k[0, i * block:(i + 1) * block] * 2.0 ** -i
+    v[0, 7 * block:8 * block] = 0
+    cache = make_cache(ctx, 10, heads, dim, block, fmt)
+    table, dtable = make_table(rng, [n], block, 10, 10, ctx.device)
+    pool = ref.Pool(10, heads, block, dim, fmt)
+    zero = torch.zeros(1, dtype=torch.int32, device=ctx.device)
+    ctx.kv_cache_append(cache, k.to(ctx.device), v.to(ctx.device), dtable, zero)
+    for m, x in (("k", k), ("v", v)):
+        pool.append(m, table[0], 0, x[0, :, 0].double().numpy(), 0)
+    dlen = torch.tensor([n], dtype=torch.int32, device=ctx.device)
+    for tokens, group in ((1, 4), (40, 3)):
+        run_attention(ctx, rng, [n], tokens, None, group, 1, dim, block, fmt, "bf16", True,
+                      state=(cache, pool, table, dtable, dlen))
+
+
+@pytest.mark.parametrize("tokens", [1, 150])
+def test_attention_peaked_and_large_queries(ctx, tokens):
+    """One key takes everything, and logits beyond what a 16-bit float holds."""
+    rng = np.random.default_rng(9)
+    for qscale, scale in ((40.0, 0.0), (3000.0, 2.0 ** -12), (1e-4, 0.0)):
+        run_attention(ctx, rng, [500, 31 + tokens], tokens, None, 4, 2, 64, 32, "int8", "bf16", True, qscale=qscale,
+                      scale=scale)
+
+
+def test_attention_accumulates_in_place_and_repeats_bit_for_bit(ctx):
+    rng = np.random.default_rng(11)
+    lengths = [900, 64, 2049]
+    cache, pool, table, dtable, dlen = filled(ctx, rng, lengths, 2, 128, 64, "int8", "bf16")
+    for tokens in (1, 70):
+        q = normals(rng, (3, tokens, 8, 128), "bf16").to(ctx.device)
+        a = torch.zeros((3, 2, 2049), device=ctx.device)
+        one = ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=a)
+        b = a.clone()
+        two = ctx.kv_cache_attention(cache, q, dtable, dlen, weights_in=b, weights_out=b)
+        ctx.check()
+        assert torch.equal(one, two)
+        assert torch.equal(b, a + a)
+        # every query spreads a weight of one
+        n = torch.minimum(dlen, torch.tensor(tokens, device=ctx.device)) if tokens > 64 else torch.full_like(dlen, tokens)
+        assert torch.allclose(a.sum((1, 2)), n.float() * 8, rtol=1e-4)
+
+
+# ---- eviction ----------------------------------------------------------------------------------
+def check_evict(ctx, rng, lengths, heads, dim, block, fmt, budget, first, last, in_place, weights=None):
+    cache, pool, table, dtable, dlen = filled(ctx, rng, lengths, heads, dim, block, fmt, "bf16", extra_pages=2 + len(lengths) * ((budget + block - 1) // block))
+    B, width = len(lengths), max(1, max(lengths)) + 5
+    w = np.exp(2 * rng.standard_normal((B, heads, width))).astype(np.float32) if weights is None else weights(B, heads, width)
+    need = (budget + block - 1) // block
+    free = sorted(set(range(cache.pages)) - set(int(p) for b, n in enumerate(lengths) for p in table[b, :(n + block - 1) // block]))
+    if not in_place:
+        to = np.array(free[:B * need], dtype=np.int32).reshape(B, need)
+        dto = torch.from_numpy(to).to(ctx.device)
+    else:
+        to, dto = table, None
+    dw = torch.from_numpy(w).to(ctx.device)
+    untouched = {m: (getattr(cache, m).clone(), getattr(cache, m + "_scale").clone()) for m in "kv"}
+    w_out = torch.full((B, heads, budget), 7.0, device=ctx.device)
+    kept, nlen, w_out = ctx.kv_cache_evict(cache, dw, dtable, dlen, budget, first, last, dst_table=dto, weights_out=w_out)
+    ctx.check()
+    got = ref.Pool.of(cache)
+    kept, nlen, w_out = kept.cpu().numpy(), nlen.cpu().numpy(), w_out.cpu().numpy()
+    written = set()
+    for b, length in enumerate(lengths):
+        n = min(length, budget)
+        assert nlen[b] == n
+        for h in range(heads):
+            want = ref.survivors(w[b, h, :length], budget, first, last)
+            assert kept[b, h, :n].tolist() == want and np.all(kept[b, h, n:] == -1), (b, h)
+            assert np.array_equal(w_out[b, h, :n], w[b, h, want], equal_nan=True) and np.all(w_out[b, h, n:] == 7.0)
+            for m in "kv":
+                new = ref.Pool(cache.pages, heads, block, dim, fmt)
+                values = pool.rows(m, table[b], want, h) if n else np.zeros((0, dim))
+                for j in range(0, n, block):
+                    part = values[j:j + block]
+                    s = ref.scale_of(float(np.abs(part).max()), fmt)
+                    pg = to[b][j // block]
+                    written.add(int(pg))
+                    assert got.scale[m][pg, h] == s
+                    assert np.array_equal(got.codes[m][pg, h, :len(part)], ref.nearest(part / s, fmt))
+    for m in "kv":   # every other page, and the rows behind the last survivor, are as they were
+        old, old_s = untouched[m]
+        rest = [p for p in range(cache.pages) if p not in written]
+        assert torch.equal(getattr(cache, m)[rest].view(torch.int8), old[rest].view(torch.int8))
+        for b, length in enumerate(lengths):
+            n = min(length, budget)
+            if n % block:
+                pg = int(to[b][n // block])
+                assert torch.equal(getattr(cache, m)[pg, :, n % block:].view(torch.int8), old[pg, :, n % block:].view(torch.int8))
+    return kept
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("block,dim,budget,first,last", [(16, 64, 33, 1, 4), (64, 128, 64, 0, 0), (32, 64, 100, 4, 96),
+                                                         (128, 128, 200, 3, 50), (16, 128, 1, 0, 0), (16, 64, 7, 7, 0)])
+def test_evict(ctx, in_place, fmt, block, dim, budget, first, last):
+    rng = np.random.default_rng(budget)
+    check_evict(ctx, rng, [0, 1, budget - 1, budget, budget + 1, 2 * budget + 300], 2, dim, block, fmt, budget, first, last, in_place)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_ties_and_odd_weights(ctx, in_place):
+    rng = np.random.default_rng(2)
+
+    def weights(B, heads, width):
+        w = rng.integers(0, 4, (B, heads, width)).astype(np.float32)      # many ties
+        w[:, :, 3::7] = np.nan
+        w[:, :, 5::11] = -0.0
+        w[:, :, 1::13] = np.inf
+        w[:, :, 2::17] = -np.inf
+        w[0, 0, :] = 0.5
+        w[1, 1, :] = np.nan
+        return w
+
+    check_evict(ctx, rng, [400, 300, 333, 90], 2, 64, 32, "int8", 128, 2, 16, in_place, weights)
+
+
+def test_evict_long(ctx):
+    rng = np.random.default_rng(4)
+    check_evict(ctx, rng, [9001, 5000], 1, 64, 64, "e4m3", 4001, 4, 100, False)
+    check_evict(ctx, rng, [9001], 1, 64, 64, "int8", 8999, 0, 1, True)
+
+
+# ---- one after the other -----------------------------------------------------------------------
+@pytest.mark.parametrize("fmt,dtype", [("int8", "bf16"), ("e4m3", "fp16")])
+def test_a_conversation(ctx, fmt, dtype):
+    """Prompt, steps with the weights added up, a cut of the cache whenever it is over its budget, more steps: the
+    state follows the definitions bit for bit and every step's output is within its bound."""
+    rng = np.random.default_rng(21)
+    heads, kv, dim, block, B = 6, 2, 64, 16, 3
+    prompt, limit, budget = [40, 7, 65], 80, 48
+    columns = (limit + block) // block
+    pages = B * columns + 4
+    cache = make_cache(ctx, pages, kv, dim, block, fmt)
+    table, dtable = make_table(rng, [columns * block] * B, block, pages, columns, ctx.device)
+    pool = ref.Pool(pages, kv, block, dim, fmt)
+    w = torch.zeros((B, kv, columns * block), device=ctx.device)
+    lens = [0] * B
+    evictions = 0
+    for step in range(30):
+        counts = prompt if step == 0 else [1] * B
+        n = max(counts)
+        q, k, v = (normals(rng, (B, n, h, dim), dtype) for h in (heads, kv, kv))
+        qd, kd, vd = as_views(ctx, q, k, v)
+        dcounts = torch.tensor(counts, dtype=torch.int32, device=ctx.device)
+        dlen = torch.tensor(lens, dtype=torch.int32, device=ctx.device)
+        ctx.kv_cache_append(cache, kd, vd, dtable, dlen, counts=dcounts)
+        dlen = dlen + dcounts
+        before = w.cpu().double().numpy()
+        out = ctx.kv_cache_attention(cache, qd, dtable, dlen, counts=dcounts, weights_in=w, weights_out=w)
+        ctx.check()
+        for b in range(B):
+            for h in range(kv):
+                pool.append("k", table[b], lens[b], k[b, :counts[b], h].double().numpy(), h)
+                pool.append("v", table[b], lens[b], v[b, :counts[b], h].double().numpy(), h)
+        lens = [a + c for a, c in zip(lens, counts)]
+        same_state(cache, pool, table, lens)
+        for b in range(B):
+            o, _, wb, spread, reach, vmax = ref.attention(pool, table[b], q[b].double().numpy(), lens[b], counts[b],
+                                                          heads, kv, True, dim ** -0.5)
+            err = np.abs(out[b, :counts[b]].cpu().double().numpy() - o)
+            assert np.all(err <= bounds(o, spread, reach, vmax, dim, lens[b], dtype))
+            got = w[b, :, :lens[b]].cpu().double().numpy()
+            want = before[b, :, :lens[b]] + wb
+            assert np.all(np.abs(got - want) <= 1e-4 * wb + 2.0 ** -23 * want + 1e-30)
+        if max(lens) > limit - 2:
+            evictions += 1
+            host = w.cpu().numpy()
+            kept, nlen, w_new = ctx.kv_cache_evict(cache, w, dtable, dlen, budget, keep_first=2, keep_last=8)
+            ctx.check()
+            for b in range(B):
+                m = min(lens[b], budget)
+                for h in range(kv):
+                    want = ref.survivors(host[b, h, :lens[b]], budget, 2, 8)
+                    assert kept[b, h, :m].tolist() == want
+                    for x in "kv":
+                        values = pool.rows(x, table[b], want, h)
+                        for j in range(0, m, block):
+                            pool.append(x, table[b], j, values[j:j + block], h)
+                lens[b] = m
+            w.zero_()
+            w[:, :, :budget] = w_new
+            same_state(cache, pool, table, lens)
+    assert evictions >= 1
+
+
+# ---- how it is called --------------------------------------------------------------------------
+def test_bad_pages_and_lengths_are_latched(ctx):
+    """Found by the kernels' own bounds checks; the cache and the outputs stay inside their buffers, and the context
+    is usable afterwards."""
+    import paper_2601_12150_b200 as spv
+    rng = np.random.default_rng(6)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [70, 40], 2, 64, 16, "int8", "bf16")
+    q = normals(rng, (2, 3, 4, 64), "bf16").to(ctx.device)
+    k = normals(rng, (2, 3, 2, 64), "bf16").to(ctx.device)
+    w = torch.ones((2, 2, 80), device=ctx.device)
+    big_q = normals(rng, (2, 90, 4, 64), "bf16").to(ctx.device)
+    spare = torch.full((2, 2), cache.pages + 5, dtype=torch.int32, device=ctx.device)
+
+    def calls(t, n):
+        yield lambda: ctx.kv_cache_attention(cache, q, t, n, weights_in=w, weights_out=w.clone())
+        yield lambda: ctx.kv_cache_attention(cache, big_q, t, n)
+        yield lambda: ctx.kv_cache_read(cache, t, n, rows=80)
+        yield lambda: ctx.kv_cache_evict(cache, w, t, n, 20)
+        yield lambda: ctx.kv_cache_append(cache, k, k, t, n)
+
+    for bad in (-1, cache.pages, 2 ** 31 - 1, -2 ** 31):
+        t = dtable.clone()
+        t[0, 0], t[0, 4], t[1, 2] = bad, bad, bad
+        for call in calls(t, dlen):
+            call()
+            with pytest.raises(spv.SpvError) as e:
+                ctx.check()
+            assert e.value.status == spv.ERR_INVALID_ARG
+    for bad in (-1, 97, 2 ** 31 - 1, -2 ** 31):
+        n = dlen.clone()
+        n[1] = bad
+        for call in calls(dtable.clamp(0, cache.pages - 1), n):
+            call()
+            with pytest.raises(spv.SpvError) as e:
+                ctx.check()
+            assert e.value.status == spv.ERR_INVALID_ARG
+    ctx.kv_cache_evict(cache, w, dtable, dlen, 20, dst_table=spare)
+    with pytest.raises(spv.SpvError):
+        ctx.check()
+    counts = torch.tensor([4, -1], dtype=torch.int32, device=ctx.device)
+    ctx.kv_cache_attention(cache, q, dtable, dlen, counts=counts)
+    with pytest.raises(spv.SpvError):
+        ctx.check()
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [70, 40], 2, 64, 16, "int8", "bf16")
+    run_attention(ctx, rng, [70, 40], 3, None, 4, 2, 64, 16, "int8", "bf16", True, state=(cache, pool, table, dtable, dlen))
+
+
+@pytest.mark.parametrize("tokens", [1, 100])
+def test_two_captured_graphs(ctx, tokens):
+    """A step captured twice, for two sequences' buffers, replayed in turn: each equals the direct call."""
+    rng = np.random.default_rng(13)
+    steps, alive = [], []
+    for i in range(2):
+        length = 300 + 200 * i
+        cache, pool, table, dtable, dlen = filled(ctx, rng, [length], 2, 64, 32, "int8", "bf16", room=tokens)
+        q, k, v = (normals(rng, (1, tokens, h, 64), "bf16").to(ctx.device) for h in (8, 2, 2))
+        w_in = torch.rand((1, 2, length + tokens), device=ctx.device)
+        w_out, out = torch.zeros_like(w_in), torch.zeros_like(q)
+
+        def step(cache=cache, q=q, k=k, v=v, dtable=dtable, dlen=dlen, w_in=w_in, w_out=w_out, out=out):
+            ctx.kv_cache_append(cache, k, v, dtable, dlen)
+            n = dlen + tokens
+            ctx.kv_cache_attention(cache, q, dtable, n, weights_in=w_in, weights_out=w_out, out=out)
+
+        step()
+        ctx.check()
+        want = (out.clone(), w_out.clone())
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step()
+        steps.append((graph, out, w_out, want))
+        alive.append(step)                           # a graph does not own the tensors that it was captured with
+    for _ in range(2):
+        for graph, out, w_out, _ in steps:
+            out.zero_()
+            w_out.zero_()
+        for graph, *_ in steps:
+            graph.replay()
+        torch.cuda.synchronize()
+        ctx.check()
+        for _, out, w_out, want in steps:
+            assert torch.equal(out, want[0]) and torch.equal(w_out, want[1])
+
+
+def test_two_streams_at_once(ctx):
+    rng = np.random.default_rng(14)
+    jobs = []
+    for i in range(2):
+        cache, pool, table, dtable, dlen = filled(ctx, rng, [4000 + 700 * i], 2, 128, 64, "e4m3", "bf16")
+        q = normals(rng, (1, 1, 8, 128), "bf16").to(ctx.device)
+        w = torch.zeros((1, 2, 5000), device=ctx.device)
+        want = ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w).clone()
+        jobs.append((cache, q, dtable, dlen, want, w.clone(), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(20):
+        for cache, q, dtable, dlen, want, w, s in jobs:
+            out, got = torch.empty_like(q), torch.zeros_like(w)
+            s.wait_stream(torch.cuda.current_stream())
+            ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=got, out=out, stream=s)
+            results.append((out, got, want, w))
+    torch.cuda.synchronize()
+    ctx.check()
+    for out, got, want, w in results:
+        assert torch.equal(out, want) and torch.equal(got, w)
+
+
+def test_refusals(ctx):
+    import paper_2601_12150_b200 as spv
+    rng = np.random.default_rng(15)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [20, 30], 2, 64, 16, "int8", "bf16")
+    q = torch.zeros((2, 1, 4, 64), dtype=torch.bfloat16, device=ctx.device)
+    k = torch.zeros((2, 1, 2, 64), dtype=torch.bfloat16, device=ctx.device)
+    w = torch.zeros((2, 2, 40), device=ctx.device)
+    small = torch.empty(256, dtype=torch.uint8, device=ctx.device)
+
+    def refused(f, status=spv.ERR_INVALID_ARG):
+        with pytest.raises(spv.SpvError) as e:
+            f()
+        assert e.value.status == status
+
+    refused(lambda: ctx.kv_cache_attention(cache, q.float(), dtable, dlen), spv.ERR_UNSUPPORTED)
+    refused(lambda: ctx.kv_cache_attention(cache, q[:, :, :3], dtable, dlen))
+    refused(lambda: ctx.kv_cache_attention(cache, q[:1], dtable, dlen))
+    refused(lambda: ctx.kv_cache_attention(cache, torch.zeros((2, 1, 4, 128), dtype=torch.bfloat16, device=ctx.device), dtable, dlen))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable.long(), dlen))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen.long()))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable[:1].expand(2, -1), dlen))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, weights_in=w))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w[:, :1].expand(2, 2, 40)))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w.double()))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, out=q[:1].expand(2, 1, 4, 64)))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, scale=-1.0))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, scale=float("nan")))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, max_length=10 ** 6))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, counts=dlen[:1]))
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w, workspace=small[:128]), spv.ERR_WORKSPACE)
+    odd = torch.zeros(2 * 4 * 65 + 8, dtype=torch.bfloat16, device=ctx.device)
+    refused(lambda: ctx.kv_cache_attention(cache, odd[1:513].view(2, 1, 4, 64), dtable, dlen), spv.ERR_ALIGNMENT)
+    refused(lambda: ctx.kv_cache_attention(cache, odd[:2 * 4 * 65].view(2, 1, 4, 65)[..., :64], dtable, dlen), spv.ERR_ALIGNMENT)
+    refused(lambda: ctx.kv_cache_append(cache, k, k.half(), dtable, dlen))
+    refused(lambda: ctx.kv_cache_append(cache, q, q, dtable, dlen))
+    refused(lambda: ctx.kv_cache_append(cache, k.float(), k.float(), dtable, dlen), spv.ERR_UNSUPPORTED)
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 0))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 10, keep_first=8, keep_last=3))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 10, dst_table=dtable))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 40, dst_table=dtable[:, :2].clone()))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 40, weights_out=w))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 10, new_lengths=dlen))
+    refused(lambda: ctx.kv_cache_evict(cache, w, dtable, dlen, 10, workspace=small), spv.ERR_WORKSPACE)
+    refused(lambda: ctx.kv_cache_evict(cache, w[:1], dtable, dlen, 10))
+    refused(lambda: ctx.kv_cache_read(cache, dtable, dlen, k_out=k.double()))
+    refused(lambda: spv.KvCache(cache.k, cache.v[:1], cache.k_scale, cache.v_scale))
+    refused(lambda: spv.KvCache(cache.k.view(torch.uint8), cache.v, cache.k_scale, cache.v_scale))
+    refused(lambda: spv.KvCache(cache.k, cache.v, cache.k_scale.double(), cache.v_scale))
+    refused(lambda: spv.KvCache(cache.k.cpu(), cache.v.cpu(), cache.k_scale.cpu(), cache.v_scale.cpu()))
+    ctx.check()
+    before = ctx.launch_count()
+    ctx.kv_cache_append(cache, k, k, dtable.clamp(0, cache.pages - 1), dlen)
+    assert ctx.launch_count() > before
+    ctx.check()

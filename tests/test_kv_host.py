@@ -1,0 +1,192 @@
+"""What of the 8-bit cache runs without a GPU: refusals, workspace sizes, and the kernels' index arithmetic with
+numbers that no caller should pass."""
+import ctypes as C
+import os
+import random
+import subprocess
+
+import numpy as np
+import pytest
+
+import kv_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 0x1000   # a pointer that is never followed: every call below is refused, or only sizes something
+
+
+def spv():
+    import paper_2601_12150_b200 as m
+    return m
+
+
+def cache(**over):
+    d = dict(pages=8, kv_heads=2, head_dim=64, block=16, format=0, k=P, v=P, k_scale=P, v_scale=P)
+    d.update(over)
+    return spv().KvCacheStruct(*d.values())
+
+
+def seqs(**over):
+    d = dict(batch=2, columns=4, table_stride=0, page_table=P, lengths=P, max_length=0)
+    d.update(over)
+    return spv().KvSeqs(*d.values())
+
+
+def attn(**over):
+    d = dict(tokens=1, heads=4, dtype=0, causal=1, softmax_scale=0.0, qb=256, qt=256, qh=64, ob=256, ot=256, oh=64, wb=128,
+             wh=64, counts=None)
+    d.update(over)
+    return spv().KvAttnDesc(*d.values())
+
+
+def evict(**over):
+    d = dict(budget=20, keep_first=1, keep_last=2, wb=128, wh=64, dst=None, dst_stride=0)
+    d.update(over)
+    return spv().KvEvictDesc(*d.values())
+
+
+def attn_size(c=None, s=None, d=None, weights=1):
+    need = C.c_size_t(0)
+    st = spv().lib().spv_kv_attention_workspace_size(C.byref(c or cache()), C.byref(s or seqs()), C.byref(d or attn()),
+                                                     weights, C.byref(need))
+    return st, need.value
+
+
+def evict_size(c=None, s=None, d=None):
+    need = C.c_size_t(0)
+    st = spv().lib().spv_kv_evict_workspace_size(C.byref(c or cache()), C.byref(s or seqs()), C.byref(d or evict()), C.byref(need))
+    return st, need.value
+
+
+def test_workspace_sizes():
+    assert attn_size()[0] == 0 and attn_size()[1] > 0
+    st, need = evict_size()
+    assert st == 0 and need >= 2 * 2 * 2 * 2 * 16 * 64
+    assert evict_size(d=evict(dst=2 * P)) == (0, 0)
+
+
+def test_refused_without_a_device():
+    m = spv()
+    inv, uns, ali = m.ERR_INVALID_ARG, m.ERR_UNSUPPORTED, m.ERR_ALIGNMENT
+    for over, status in [(dict(pages=0), inv), (dict(kv_heads=0), inv), (dict(head_dim=80), uns), (dict(block=48), uns),
+                         (dict(format=2), inv), (dict(k=None), inv), (dict(v_scale=None), inv), (dict(k=P + 8), ali),
+                         (dict(pages=1 << 30, kv_heads=16), uns)]:
+        assert attn_size(c=cache(**over))[0] == status and evict_size(c=cache(**over))[0] == status, over
+    for over, status in [(dict(batch=0), inv), (dict(columns=0), inv), (dict(page_table=None), inv), (dict(lengths=None), inv),
+                         (dict(table_stride=3), inv), (dict(table_stride=-4), inv), (dict(max_length=65), inv),
+                         (dict(max_length=-1), inv), (dict(batch=70000), uns), (dict(columns=1 << 29), uns)]:
+        assert attn_size(s=seqs(**over))[0] == status and evict_size(s=seqs(**over))[0] == status, over
+    for over, status in [(dict(tokens=0), inv), (dict(heads=3), inv), (dict(heads=0), inv), (dict(dtype=2), uns),
+                         (dict(causal=2), inv), (dict(softmax_scale=-1.0), inv), (dict(softmax_scale=float("nan")), inv),
+                         (dict(softmax_scale=float("inf")), inv), (dict(qt=260), ali), (dict(oh=65), ali), (dict(wb=-1), inv),
+                         (dict(tokens=1 << 29, heads=4), uns)]:
+        assert attn_size(d=attn(**over))[0] == status, over
+    for over, status in [(dict(budget=0), inv), (dict(keep_first=-1), inv), (dict(keep_first=15, keep_last=6), inv),
+                         (dict(budget=65), inv), (dict(dst=P), inv), (dict(dst=2 * P, dst_stride=1), inv),
+                         (dict(keep_first=2 ** 31 - 1, keep_last=2 ** 31 - 1), inv)]:
+        assert evict_size(d=evict(**over))[0] == status, over
+    lib = m.lib()
+    need = C.c_size_t(0)
+    assert lib.spv_kv_attention_workspace_size(None, None, None, 0, C.byref(need)) == inv
+    a = m.KvAppendDesc(1, 0, 256, 128, 64, None)
+    r = m.KvReadDesc(4, 0, 256, 128, 64, None)
+
+    def append(desc, k=P):
+        return lib.kv_cache_append(None, C.byref(cache()), C.byref(seqs()), C.byref(desc), k, P, None)
+
+    def read(desc, k=P):
+        return lib.kv_cache_read(None, C.byref(cache()), C.byref(seqs()), C.byref(desc), k, None, None)
+
+    assert append(a) == inv and read(r) == inv                       # no context
+    assert append(m.KvAppendDesc(1, 2, 256, 128, 64, None)) == uns and append(m.KvAppendDesc(0, 0, 8, 8, 8, None)) == inv
+    assert append(m.KvAppendDesc(1, 0, 4, 8, 8, None)) == ali and append(a, P + 2) == ali and append(a, None) == inv
+    assert read(m.KvReadDesc(4, 3, 8, 8, 8, None)) == uns and read(m.KvReadDesc(0, 0, 8, 8, 8, None)) == inv
+    assert read(m.KvReadDesc(4, 0, 8, 12, 8, None)) == ali and read(r, None) == inv
+    assert lib.kv_cache_attention(None, C.byref(cache()), C.byref(seqs()), C.byref(attn()), P, P, None, None, None, None, 0,
+                                  None) == inv
+    assert lib.kv_cache_evict(None, C.byref(cache()), C.byref(seqs()), C.byref(evict(dst=2 * P)), 0x100000, P, None, 3 * P,
+                              None, 0, None) == inv
+
+
+@pytest.fixture(scope="module")
+def index(tmp_path_factory):
+    """The kernels' index header, compiled for the host."""
+    d = tmp_path_factory.mktemp("kv")
+    src = d / "index.cpp"
+    src.write_text('#include "%s"\nextern "C" {\n'
+                   "int clampi(int x, int m) { return spv_kv_clamp(x, m); }\n"
+                   "int valid(int p, int n) { return spv_kv_valid_page(p, n); }\n"
+                   "long long row(int p, int h, int i, int b, int s) { return spv_kv_row(p, h, i, b, s); }\n"
+                   "void span(int l, int c, int b, int t, int* o) { SpvKvSpan s = spv_kv_append_span(l, c, b, t);"
+                   " o[0] = s.column; o[1] = s.base; o[2] = s.lo; o[3] = s.hi; }\n"
+                   "int qend(int l, int n, int i, int c) { return spv_kv_query_end(l, n, i, c); }\n}\n"
+                   % os.path.join(ROOT, "paper_2601_12150_b200", "csrc", "kv_index.cuh"))
+    so = d / "index.so"
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover", "-o", str(so), str(src)],
+                   check=True)
+    lib = C.CDLL(str(so))
+    lib.row.restype = C.c_longlong
+    return lib
+
+
+WILD = [-2 ** 31, -2 ** 31 + 1, -1, 0, 1, 2, 15, 16, 17, 63, 64, 1000, 2 ** 30, 2 ** 31 - 2, 2 ** 31 - 1]
+
+
+def test_no_page_number_leads_out_of_the_pool(index):
+    for pages, heads, block in ((1, 1, 16), (7, 3, 64), (2 ** 31 // (8 * 128) - 1, 8, 128)):
+        rows = pages * heads * block
+        for p in WILD + [pages - 1, pages]:
+            if index.valid(p, pages):
+                for head in (0, heads - 1):
+                    for slot in (0, 1, block - 1, block, 12345):
+                        assert 0 <= index.row(p, heads, head, block, slot) < rows
+            else:
+                assert not 0 <= p < pages
+
+
+def test_no_length_or_count_leads_out_of_the_table(index):
+    r = random.Random(0)
+    out = (C.c_int * 4)()
+    for _ in range(3000):
+        block, columns = r.choice([16, 32, 64, 128]), r.randint(1, 9)
+        most, tokens = r.randint(1, columns * block), r.choice([1, 2, 17, 200, 100000])
+        length = index.clampi(r.choice(WILD + [r.randint(0, most)]), most)
+        count = index.clampi(index.clampi(r.choice(WILD + [r.randint(0, tokens)]), tokens), most - length)
+        assert 0 <= length <= most and 0 <= length + count <= most
+        touched = min((tokens + block - 2) // block + 1, columns)
+        seen = []
+        for t in range(touched):
+            index.span(length, count, block, t, out)
+            column, base, lo, hi = out
+            if lo < hi:
+                assert 0 <= column < columns and base == column * block and base <= lo and hi <= base + block
+                seen += range(lo, hi)
+        assert seen == list(range(length, length + count))      # every new token once
+
+
+def test_causal_ends_stay_inside_the_sequence(index):
+    for length in (0, 1, 5, 64, 2 ** 30):
+        for n in (0, 1, 7, 2 ** 30, 2 ** 31 - 1):
+            for i in (0, 1, 6, 2 ** 30):
+                if i < max(n, 1):
+                    e = index.qend(length, n, i, 1)
+                    assert 0 <= e <= length and e == min(length, max(0, length - n + i + 1))
+                    assert index.qend(length, n, i, 0) == length
+
+
+def test_reference_scale_and_rounding():
+    """The oracle itself: the scale is the smallest that fits, and rounding is to the nearest code (ties to even)."""
+    rng = np.random.default_rng(0)
+    import torch
+    for fmt in ("int8", "e4m3"):
+        for a in list(np.exp(rng.uniform(-60, 60, 200))) + [ref.M[fmt], 2 * ref.M[fmt], 1.0]:
+            s = ref.scale_of(float(a), fmt)
+            assert a <= ref.M[fmt] * s and a > ref.M[fmt] * s / 2
+        assert ref.scale_of(0.0, fmt) == 2.0 ** -100
+        x = rng.uniform(-ref.M[fmt], ref.M[fmt], 20000)
+        x[::3] = np.float32(x[::3] / 32).astype(np.float64)
+        x = x.astype(np.float32).astype(np.float64)
+        got = ref.nearest(x, fmt)
+        if fmt == "e4m3":
+            assert np.array_equal(got, torch.from_numpy(x).float().to(torch.float8_e4m3fn).double().numpy())
+        else:
+            assert np.all(np.abs(got - x) <= 0.5)
