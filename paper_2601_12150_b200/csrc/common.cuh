@@ -29,6 +29,7 @@ struct spv_ctx {
   int32_t prof_on;
   // one-time per-device launch configuration (function attributes are per device, and a context is bound to one)
   int32_t attn_configured;
+  uint32_t kv_configured;              // bit per form of the cache attention
   int32_t gemm_single_configured[8];   // per epilogue variant
   int32_t gemm_max_pairs[8];     // per epilogue variant: CTA pairs of the pair-form GEMM that can be resident at
                                  // once (0 = not yet queried)
@@ -97,6 +98,10 @@ int32_t spv_make_tmap_bf16(spv_ctx* ctx, CUtensorMap* map, const void* base, int
 int32_t spv_make_tmap_f32(spv_ctx* ctx, CUtensorMap* map, const void* base, int rank,
                           const uint64_t* dims, const uint64_t* strides_bytes,
                           const uint32_t* box);
+
+// Same for byte tensors (box rows of 128 bytes).
+int32_t spv_make_tmap_u8(spv_ctx* ctx, CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
+                         const uint64_t* strides_bytes, const uint32_t* box);
 
 static inline size_t spv_align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

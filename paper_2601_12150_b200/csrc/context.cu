@@ -188,3 +188,8 @@ int32_t spv_make_tmap_f32(spv_ctx* ctx, CUtensorMap* map, const void* base, int 
                           const uint64_t* strides_bytes, const uint32_t* box) {
   return make_tmap(ctx, map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, base, rank, dims, strides_bytes, box);
 }
+
+int32_t spv_make_tmap_u8(spv_ctx* ctx, CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
+                         const uint64_t* strides_bytes, const uint32_t* box) {
+  return make_tmap(ctx, map, CU_TENSOR_MAP_DATA_TYPE_UINT8, base, rank, dims, strides_bytes, box);
+}

@@ -5,25 +5,11 @@
 //                          the queries and the heads of a key head in a fixed order.
 #include <type_traits>
 
-#include "kv_cache.cuh"
+#include "kv_attention.cuh"
 
 namespace {
 
 using namespace spv;
-
-struct AttnArgs {
-  const uint16_t* q;
-  uint16_t* o;
-  float* lse;
-  const float* w_in;
-  float* w_out;
-  const int32_t* counts;
-  int64_t q_stride_b, q_stride_tok, q_stride_head;
-  int64_t o_stride_b, o_stride_tok, o_stride_head;
-  int64_t w_stride_b, w_stride_head;
-  int32_t tokens, heads, group, block, causal, max_length;
-  float scale;
-};
 
 // <q, codes of a row> in fp32, from shared memory and a row of the pool.
 template <int FMT, int D>
@@ -45,7 +31,7 @@ __device__ __forceinline__ float row_dot(const float* q, const uint8_t* row) {
 }
 
 template <int FMT, int DT, int D>
-__global__ void __launch_bounds__(128) kv_attn_row_kernel(KvView c, AttnArgs a) {
+__global__ void __launch_bounds__(128) kv_attn_row_kernel(KvView c, KvAttnArgs a) {
   __shared__ float qs[D];
   __shared__ float ps[128];
   __shared__ float red[8];
@@ -115,7 +101,7 @@ __global__ void __launch_bounds__(128) kv_attn_row_kernel(KvView c, AttnArgs a) 
 }
 
 template <int FMT, int DT, int D>
-__global__ void __launch_bounds__(128) kv_attn_weight_kernel(KvView c, AttnArgs a) {
+__global__ void __launch_bounds__(128) kv_attn_weight_kernel(KvView c, KvAttnArgs a) {
   __shared__ float qs[D];
   __shared__ float s_lse;
   const int b = blockIdx.z, hk = blockIdx.y, j = blockIdx.x * 128 + threadIdx.x;
@@ -162,6 +148,11 @@ int32_t check_attn(const spv_kv_cache* c, const spv_kv_seqs* s, const spv_kv_att
   return SPV_OK;
 }
 
+// Whether the streaming form takes the call: few enough rows share a key head.
+bool streams(const spv_kv_cache* c, const spv_kv_attn_desc* d) {
+  return (int64_t)d->tokens * (d->heads / c->kv_heads) <= kKvStreamMaxRows;
+}
+
 }  // namespace
 
 extern "C" int32_t spv_kv_attention_workspace_size(const spv_kv_cache* cache, const spv_kv_seqs* seqs,
@@ -169,7 +160,8 @@ extern "C" int32_t spv_kv_attention_workspace_size(const spv_kv_cache* cache, co
   const int32_t st = check_attn(cache, seqs, d);
   if (st != SPV_OK) return st;
   if (!bytes) return SPV_ERR_INVALID_ARG;
-  *bytes = want_weights ? spv_align_up((size_t)seqs->batch * d->tokens * d->heads * sizeof(float), 256) : 0;
+  if (streams(cache, d)) *bytes = spv_kv_stream_workspace(cache, seqs, d, want_weights != 0);
+  else *bytes = want_weights ? spv_align_up((size_t)seqs->batch * d->tokens * d->heads * sizeof(float), 256) : 0;
   return SPV_OK;
 }
 
@@ -187,7 +179,7 @@ extern "C" int32_t kv_cache_attention(spv_ctx* ctx, const spv_kv_cache* cache, c
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 255u))) return SPV_ERR_WORKSPACE;
   cudaStream_t stream = (cudaStream_t)stream_;
   const KvView view = kv_view(ctx, cache, seqs);
-  AttnArgs a;
+  KvAttnArgs a;
   a.q = (const uint16_t*)q;
   a.o = (uint16_t*)o;
   a.lse = lse ? lse : (float*)(weights_out ? workspace : nullptr);
@@ -197,14 +189,19 @@ extern "C" int32_t kv_cache_attention(spv_ctx* ctx, const spv_kv_cache* cache, c
   a.q_stride_b = d->q_stride_b; a.q_stride_tok = d->q_stride_tok; a.q_stride_head = d->q_stride_head;
   a.o_stride_b = d->o_stride_b; a.o_stride_tok = d->o_stride_tok; a.o_stride_head = d->o_stride_head;
   a.w_stride_b = d->w_stride_b; a.w_stride_head = d->w_stride_head;
+  a.batch = seqs->batch;
   a.tokens = d->tokens;
   a.heads = d->heads;
   a.group = d->heads / cache->kv_heads;
   a.block = cache->block;
   a.causal = d->causal;
-  a.max_length = view.max_length;
+  a.dtype = d->dtype;
   a.scale = d->softmax_scale > 0.0f ? d->softmax_scale : 1.0f / sqrtf((float)cache->head_dim);
   SpvProfScope prof(ctx, SPV_K_KV_ATTN, stream);
+  if (streams(cache, d)) {
+    a.lse = lse;
+    return spv_kv_stream_run(ctx, cache, seqs, a, workspace, stream);
+  }
   const dim3 rows(d->tokens * d->heads, 1, seqs->batch);
   const dim3 keys((view.max_length + 127) / 128, cache->kv_heads, seqs->batch);
   auto launch = [&](auto fmt, auto dt, auto dim) {

@@ -1,0 +1,68 @@
+// Shared by the attention kernels over the 8-bit cache: arguments, 8-bit -> fp16 conversions, warp-level products.
+#pragma once
+#include "kv_cache.cuh"
+
+struct KvAttnArgs {
+  const uint16_t* q;
+  uint16_t* o;
+  float* lse;              // natural log, packed [batch, tokens, heads]; may be NULL
+  const float* w_in;
+  float* w_out;
+  const int32_t* counts;
+  int64_t q_stride_b, q_stride_tok, q_stride_head;
+  int64_t o_stride_b, o_stride_tok, o_stride_head;
+  int64_t w_stride_b, w_stride_head;
+  int32_t batch, tokens, heads, group, block, causal, dtype;
+  float scale;
+};
+
+// ---- the streaming form (few query rows per key head), kv_attention_stream.cu ----
+constexpr int kKvStreamMaxRows = 32;      // query rows (queries x heads of a key head) it takes
+size_t spv_kv_stream_workspace(const spv_kv_cache* cache, const spv_kv_seqs* seqs, const spv_kv_attn_desc* d, bool weights);
+int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs, const KvAttnArgs& a,
+                          void* workspace, cudaStream_t stream);
+
+#ifdef __CUDACC__
+namespace spv {
+
+// Four codes -> two fp16 pairs, exactly.
+// int8: with the sign bit flipped a code x is the byte x + 128, and 0x6400 | byte is the fp16 number 1024 + 128 + x.
+template <int FMT>
+__device__ __forceinline__ void kv_half4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (FMT == SPV_KV_INT8) {
+    const uint32_t x = w ^ 0x80808080u;
+    const __half2 bias = __half2half2(__ushort_as_half(0x6480));   // 1152
+    uint32_t a = __byte_perm(x, 0x64646464u, 0x4140), b = __byte_perm(x, 0x64646464u, 0x4342);
+    __half2 p = __hsub2(*reinterpret_cast<__half2*>(&a), bias), q = __hsub2(*reinterpret_cast<__half2*>(&b), bias);
+    lo = *reinterpret_cast<uint32_t*>(&p);
+    hi = *reinterpret_cast<uint32_t*>(&q);
+  } else {
+    const __half2_raw p = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xFFFFu), __NV_E4M3);
+    const __half2_raw q = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    lo = (uint32_t)p.x | (uint32_t)p.y << 16;
+    hi = (uint32_t)q.x | (uint32_t)q.y << 16;
+  }
+}
+
+// d += a (16 x 16) * b (16 x 8), fp16 inputs, fp32 sums
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// transpose of an 8 x 8 matrix of 16-bit values spread over a warp
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+}  // namespace spv
+#endif
