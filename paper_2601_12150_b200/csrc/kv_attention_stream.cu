@@ -2,10 +2,10 @@
 //
 // Bound by HBM: 2 * head_dim bytes a key and key head are read once, for 4 * head_dim * rows operations.
 //
-//   kv_stream_kernel  one CTA per SM.  All key tiles (64 slots) of all (sequence, key head) pairs form one line,
+//   kv_stream_kernel  one CTA per SM.  All key tiles (8 KB) of all (sequence, key head) pairs form one line,
 //                     and every CTA takes an equal stretch of it, whatever the lengths are.  A producer warp brings
 //                     the tiles in by TMA (as many in flight as shared memory holds: the latency of HBM times its
-//                     rate is 35 KB an SM); seven warps take them in turn, each with an online softmax of its own,
+//                     rate is 35 KB an SM); the other warps take them in turn, each with an online softmax of its own,
 //                     and join their states where the pair changes.  Codes go from shared memory to fp16 fragments
 //                     in registers (the 128-byte swizzle makes the 16-byte reads of both operands free of bank
 //                     conflicts), and the products run with keys as the rows: S^T = K Q^T and O^T = V^T P^T, so
@@ -24,15 +24,16 @@ namespace {
 
 using namespace spv;
 
-constexpr int kTile = 64;                    // slots of a key tile
-constexpr int kWarps = 7;                    // consumer warps (with the producer two a scheduler: 255 registers a thread)
-constexpr int kStreamThreads = (kWarps + 1) * 32;
+// slots of a key tile: 8 KB of keys and values
+__host__ __device__ constexpr int tile_of(int head_dim) { return head_dim == 128 ? 32 : 64; }
+constexpr int kMergeWarps = 8;               // warps whose results are added up at a time
 constexpr int kPartSlots = 2;                // pieces a CTA can leave: of the pair it began in, of the one it ended in
 constexpr float kLazy = 8.0f;
+constexpr int kIssue = 4;                    // tiles that the producer's lanes bring in side by side
 
 struct StreamArgs {
   KvAttnArgs a;
-  float* z;             // scores (log2 domain) [tile][rows][64], NULL when no weights are wanted
+  float* z;             // scores (log2 domain) [tile][rows][slot], NULL when no weights are wanted
   float* part_o;        // [CTA][2][8 NT][D] unnormalised
   float2* part_ml;      // [CTA][2][8 NT] maximum, sum
   float2* pair_ml;      // [pair][8 NT]: the same of pairs that one CTA had whole
@@ -47,15 +48,25 @@ struct StageMeta {      // of one tile, by 16-slot quarters
 
 template <int D, int NT>
 struct Layout {
+  // place of tile `it` of the CTA, and the phase of that stage's barriers
+  __device__ static int stage(uint32_t it) { return (int)(it % kWarps * kOwn + it / kWarps % kOwn); }
+  __device__ static uint32_t phase(uint32_t it) { return it / kWarps / kOwn; }
+  static constexpr int kTile = tile_of(D);
+  // consumer warps: with the producer 3 or 2 a scheduler, which leaves 168 or 255 registers a thread
+  static constexpr int kWarps = NT < 4 ? 11 : 7;
+  static constexpr int kThreads = (kWarps + 1) * 32;
   static constexpr int kStageBytes = 2 * kTile * D;
   static constexpr int kMergePitch = D + 4;
-  static constexpr int kMerge = kWarps * 8 * kMergePitch * 4;
+  static constexpr int kMerge = kMergeWarps * 8 * kMergePitch * 4;
   static constexpr int kQ = NT * (D / 16) * 32 * 8;
   static constexpr int kRows = 8 * NT;
   static constexpr int kSmall = kRows * 4 * 2 + kWarps * kRows * 8 + 2048;
   static constexpr int kBudget = 227 * 1024 - 1024;
   static constexpr int kFit = (kBudget - kMerge - kQ - kSmall) / (kStageBytes + (int)sizeof(StageMeta) + 16);
-  static constexpr int kStages = kFit > 24 ? 24 : kFit;
+  // Stages belong to one consumer warp each, which waits for their phases one after the other: a parity says which of
+  // two phases is over, so nobody may wait for a phase while the one before it is still to come.
+  static constexpr int kOwn = kFit / kWarps;
+  static constexpr int kStages = kOwn * kWarps;
   static constexpr int oMerge = kStages * kStageBytes;
   static constexpr int oQ = oMerge + kMerge;
   static constexpr int oMeta = oQ + kQ;
@@ -70,7 +81,7 @@ struct Layout {
 // ---- the line of tiles -------------------------------------------------------------------------
 struct Scan {
   int64_t total, before;     // tiles of all sequences; of those before the one that holds the target
-  int64_t warp_sum[kWarps + 1];
+  int64_t warp_sum[16];
   int b;
 };
 
@@ -78,17 +89,18 @@ __device__ __forceinline__ int seq_len(const KvView& c, int b) { return spv_kv_c
 __device__ __forceinline__ int seq_queries(const KvAttnArgs& a, int b) {
   return a.counts ? spv_kv_clamp(__ldg(a.counts + b), a.tokens) : a.tokens;
 }
+template <int TILE>
 __device__ __forceinline__ int seq_key_tiles(const KvView& c, const KvAttnArgs& a, int b) {
-  return seq_queries(a, b) > 0 ? (seq_len(c, b) + kTile - 1) / kTile : 0;
+  return seq_queries(a, b) > 0 ? (seq_len(c, b) + TILE - 1) / TILE : 0;
 }
 
 // Sums the tiles of all sequences; then the sequence that holds tile `share(total)`.  All threads of the CTA.
-template <int THREADS, typename F>
+template <int THREADS, int TILE, typename F>
 __device__ __forceinline__ void scan_tiles(const KvView& c, const KvAttnArgs& a, Scan* s, F share) {
   const int per = (a.batch + THREADS - 1) / THREADS;
   const int b0 = threadIdx.x * per, b1 = min(a.batch, b0 + per);
   int64_t sum = 0;
-  for (int b = b0; b < b1; ++b) sum += (int64_t)c.kv_heads * seq_key_tiles(c, a, b);
+  for (int b = b0; b < b1; ++b) sum += (int64_t)c.kv_heads * seq_key_tiles<TILE>(c, a, b);
   int64_t inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -108,7 +120,7 @@ __device__ __forceinline__ void scan_tiles(const KvView& c, const KvAttnArgs& a,
   if (target >= at && target < at + sum) {
     int b = b0;
     for (;; ++b) {
-      const int64_t t = (int64_t)c.kv_heads * seq_key_tiles(c, a, b);
+      const int64_t t = (int64_t)c.kv_heads * seq_key_tiles<TILE>(c, a, b);
       if (target < at + t || b + 1 >= b1) break;
       at += t;
     }
@@ -134,13 +146,14 @@ struct Walk {
   int64_t pos, end, before;
   int b;
 };
+template <int TILE>
 __device__ __forceinline__ bool next_piece(const KvView& c, const KvAttnArgs& a, Walk& w, Piece& p) {
   if (w.pos >= w.end) return false;
-  int tiles = seq_key_tiles(c, a, w.b);
+  int tiles = seq_key_tiles<TILE>(c, a, w.b);
   while (w.pos >= w.before + (int64_t)c.kv_heads * tiles) {
     w.before += (int64_t)c.kv_heads * tiles;
     if (++w.b >= a.batch) return false;
-    tiles = seq_key_tiles(c, a, w.b);
+    tiles = seq_key_tiles<TILE>(c, a, w.b);
   }
   const int off = (int)(w.pos - w.before);
   p.b = w.b;
@@ -180,7 +193,7 @@ template <int D, int NT>
 __device__ __forceinline__ void load_queries(const StreamArgs& s, const Piece& p, uint16_t* q, float* factor, int* ends) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int kPer = D / 32;     // elements of a row for each lane
-  for (int row = warp; row < 8 * NT; row += kWarps) {
+  for (int row = warp; row < 8 * NT; row += Layout<D, NT>::kWarps) {
     const int i = row / s.a.group, head = p.head * s.a.group + row % s.a.group;
     float x[kPer];
 #pragma unroll
@@ -219,13 +232,16 @@ __device__ __forceinline__ void load_queries(const StreamArgs& s, const Piece& p
 }
 
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(kStreamThreads, 1)
+__global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
     kv_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const KvView c,
                      const StreamArgs s) {
   using L = Layout<D, NT>;
   constexpr int kRows = L::kRows;
+  constexpr int kWarps = L::kWarps;
+  constexpr int kTile = L::kTile;
+  constexpr int kQuarters = kTile / 16;        // scales are kept for 16 slots each
   constexpr int kSteps = D / 16;             // k steps of S^T, row tiles of O^T
-  constexpr int kKeys = NT < 4 ? 64 : (D == 64 ? 32 : 16);   // keys whose scores are held at once
+  constexpr int kKeys = NT < 4 || D == 64 ? 32 : 16;   // keys whose scores are held at once
   constexpr int kMt = kKeys / 16;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -253,12 +269,12 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
     *abort_flag = 0u;
   }
   if (blockIdx.x == 0) {       // the caller's numbers: a bad one is latched once
-    for (int b = threadIdx.x; b < s.a.batch; b += kStreamThreads) {
+    for (int b = threadIdx.x; b < s.a.batch; b += L::kThreads) {
       kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
       if (s.a.counts) kv_clamped(__ldg(s.a.counts + b), s.a.tokens, c.status);
     }
   }
-  scan_tiles<kStreamThreads>(c, s.a, scan, [&](int64_t total) {
+  scan_tiles<L::kThreads, kTile>(c, s.a, scan, [&](int64_t total) {
     const int w = working_ctas(total, gridDim.x);
     return blockIdx.x < w ? stretch_begin(total, blockIdx.x, w) : total;
   });
@@ -274,65 +290,85 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
   Piece p;
 
   if (warp == kWarps) {
-    // ---- producer: lanes look up 32 page parts at a time, lane 0 issues
+    // ---- producer: every lane has a tile of its own, and kIssue lanes at a time wait, copy and describe; the page
+    // numbers of the next 32 tiles are on their way meanwhile
     uint64_t policy;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     const int part = min(s.a.block, kTile);              // slots that one copy brings
-    const int parts = kTile / part;                      // copies of a tile
-    const int quarters = 4 / parts;                      // 16-slot quarters of a part
+    const int parts = kTile / part;                      // copies of a tile: 1, 2 or 4
     uint32_t it = 0;
-    while (next_piece(c, s.a, walk, p)) {
+    while (next_piece<kTile>(c, s.a, walk, p)) {
       const int32_t* row = c.table + p.b * c.table_stride;
-      const int part_end = p.kt1 * parts;
-      for (int base = p.kt0 * parts; base < part_end; base += 32) {
-        const int mine = base + lane, slot = mine * part;
-        int page = -1;
-        bool wanted = mine < part_end && slot < p.len;
-        float ks = 0.0f, vs = 0.0f;          // of parts that hold nothing
-        if (wanted) page = kv_page(row, slot / s.a.block, c.pages, c.status);
-        if (page >= 0) {
-          const size_t ph = (size_t)page * c.kv_heads + p.head;
-          ks = __ldg(c.k_scale + ph);
-          vs = __ldg(c.v_scale + ph);
+      int next[kQuarters];
+      auto fetch = [&](int kt) {
+#pragma unroll
+        for (int x = 0; x < kQuarters; ++x) {
+          const int slot = kt * kTile + x * part;
+          next[x] = x < parts && kt < p.kt1 && slot < p.len ? __ldg(row + slot / s.a.block) : INT32_MIN;
         }
-        const int pool_row = page >= 0 ? (int)(spv_kv_row(page, c.kv_heads, p.head, s.a.block, slot) / (128 / D)) : -1;
-        const int count = min(32, part_end - base);
-        for (int j = 0; j < count; j += parts, ++it) {
-          const int st = it % L::kStages;
-          if (it >= L::kStages) mbar_wait(empty + st, ((it / L::kStages) - 1) & 1, abort_flag, wait_status, 0x4B01u);
-          uint8_t* kdst = smem + st * L::kStageBytes;
-          int loads = 0;
-          for (int x = 0; x < parts; ++x) loads += __shfl_sync(0xffffffffu, pool_row, j + x) >= 0 ? 1 : 0;
-          if (lane == 0) mbar_expect_tx(full + st, loads * 2 * part * D);
-          for (int x = 0; x < parts; ++x) {
-            const int r = __shfl_sync(0xffffffffu, pool_row, j + x);
-            if (lane == 0 && r >= 0) {
-              tma_load_rows(kdst + x * part * D, &map_k, full + st, r, policy);
-              tma_load_rows(kdst + kTile * D + x * part * D, &map_v, full + st, r, policy);
-            }
+      };
+      fetch(p.kt0 + lane);
+      for (int base = p.kt0; base < p.kt1; base += 32) {
+        const int kt = base + lane;
+        int page[kQuarters];
+        float ks[kQuarters], vs[kQuarters];
+        int loads = 0, bad = 0;
+#pragma unroll
+        for (int x = 0; x < kQuarters; ++x) {
+          page[x] = next[x];
+          ks[x] = vs[x] = 0.0f;                          // of parts that hold nothing
+          if (spv_kv_valid_page(page[x], c.pages)) {
+            const size_t ph = (size_t)page[x] * c.kv_heads + p.head;
+            ks[x] = __ldg(c.k_scale + ph);
+            vs[x] = __ldg(c.v_scale + ph);
+            ++loads;
+          } else if (x < parts && kt < p.kt1 && kt * kTile + x * part < p.len) {
+            kv_fault(c.status, SPV_SITE_KV_PAGE);
+            bad |= ((1 << kQuarters / parts) - 1) << x * (kQuarters / parts);
           }
-          StageMeta* m = meta + st;
-          const uint32_t lost = __ballot_sync(0xffffffffu, wanted && page < 0);
-          if (lane >= j && lane < j + parts) {
-            for (int x = 0; x < quarters; ++x) {
-              m->ks[(lane - j) * quarters + x] = ks;
-              m->vs[(lane - j) * quarters + x] = vs;
+        }
+        if (base + 32 < p.kt1) fetch(base + 32 + lane);
+        const int count = min(32, p.kt1 - base);
+        for (int j = 0; j < count; j += kIssue) {
+          if (lane >= j && lane < min(j + kIssue, count)) {
+            const uint32_t at = it + lane;
+            const int st = L::stage(at);
+            if (at >= L::kStages) mbar_wait(empty + st, (L::phase(at) - 1) & 1, abort_flag, wait_status, 0x4B01u);
+            uint8_t* kdst = smem + st * L::kStageBytes;
+            mbar_expect_tx(full + st, loads * 2 * part * D);
+#pragma unroll
+            for (int x = 0; x < kQuarters; ++x) {
+              if (spv_kv_valid_page(page[x], c.pages)) {
+                const int at_row = (int)(spv_kv_row(page[x], c.kv_heads, p.head, s.a.block, kt * kTile + x * part) / (128 / D));
+                tma_load_rows(kdst + x * part * D, &map_k, full + st, at_row, policy);
+                tma_load_rows(kdst + kTile * D + x * part * D, &map_v, full + st, at_row, policy);
+              }
             }
-          }
-          if (lane == 0) {
-            int bad = 0;
-            for (int x = 0; x < 4; ++x) bad |= (int)((lost >> (j + x / quarters)) & 1u) << x;
+            StageMeta* m = meta + st;
+#pragma unroll
+            for (int x = 0; x < kQuarters; ++x) {
+              const int y = x * parts / kQuarters;       // part that quarter x is in
+              float kx = ks[0], vx = vs[0];
+#pragma unroll
+              for (int i = 1; i < kQuarters; ++i) {
+                kx = y == i ? ks[i] : kx;
+                vx = y == i ? vs[i] : vx;
+              }
+              m->ks[x] = kx;
+              m->vs[x] = vx;
+            }
             m->bad = bad;
+            mbar_arrive(full + st);
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(full + st);
         }
+        it += count;
       }
     }
     // nothing of this CTA is in flight when it ends: a wait that gave up leaves copies behind
     if (*abort_flag != 0u && lane == 0) {
       for (uint32_t i = it > L::kStages ? it - L::kStages : 0; i < it; ++i)
-        for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(full + i % L::kStages, (i / L::kStages) & 1, 1000u); ++tries) {
+        for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(full + L::stage(i), L::phase(i) & 1, 1000u); ++tries) {
         }
     }
     return;
@@ -341,7 +377,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
   // ---- consumers
   const int r = lane >> 2, q2 = (lane & 3) * 2;
   uint32_t ring = 0;
-  while (next_piece(c, s.a, walk, p)) {
+  while (next_piece<kTile>(c, s.a, walk, p)) {
     load_queries<D, NT>(s, p, sq, factor, ends);
     asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
     const int full_end = ends[0];           // slots that every query sees (row 0 sees least)
@@ -369,15 +405,17 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
     }
     const uint32_t ring_end = ring + (p.kt1 - p.kt0);
     for (uint32_t it = ring + (warp + kWarps - ring % kWarps) % kWarps; it < ring_end; it += kWarps) {
-      const int st = it % L::kStages;
+      const int st = L::stage(it);
       const int kt = p.kt0 + (int)(it - ring);
-      mbar_wait(full + st, (it / L::kStages) & 1, abort_flag, wait_status, 0x4B02u);
+      mbar_wait(full + st, L::phase(it) & 1, abort_flag, wait_status, 0x4B02u);
       const uint32_t kbase = smem_u32(smem) + st * L::kStageBytes, vbase = kbase + kTile * D;
       const StageMeta* mt_at = meta + st;
       const int bad = mt_at->bad;
       const bool edge = (kt + 1) * kTile > full_end || bad != 0;
       // the unit of o follows the value scales by powers of two and more, not by every block's own
-      const float vt = fmaxf(fmaxf(mt_at->vs[0], mt_at->vs[1]), fmaxf(mt_at->vs[2], mt_at->vs[3]));
+      float vt = mt_at->vs[0];
+#pragma unroll
+      for (int x = 1; x < kQuarters; ++x) vt = fmaxf(vt, mt_at->vs[x]);
       vtop = fmaxf(vtop, vt);
       if (!(vt <= vref * 16.0f && vt >= vref * 0.0625f)) {
         const float next = fmaxf(vt, vtop * 0x1p-60f);
@@ -391,7 +429,7 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
         vref = next;
       }
       const float vinv = vref > 0.0f ? 1.0f / vref : 0.0f;
-#pragma unroll
+#pragma unroll 1     // the body once: several warps a scheduler at different places of it share its instruction cache
       for (int half = 0; half < kTile / kKeys; ++half) {
         float z[kMt][NT][4];
 #pragma unroll
@@ -579,32 +617,56 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
     const int slot = 2 * blockIdx.x + (p.kt0 > 0 ? 0 : 1);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+      constexpr int kParts = 8 * (D / 4);                              // float4s of eight queries' rows
+      constexpr int kMine = (kParts + kWarps * 32 - 1) / (kWarps * 32);
+      float4 sums[kMine];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float top = -INFINITY;
+      for (int y = 0; y < kMine; ++y) sums[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sml[w * kRows + 8 * t + q2 + e].x);
-        const float f = m[t][e] == -INFINITY ? 0.0f : exp2_fast(m[t][e] - top) * vref;
-        float* at = merge + (warp * 8 + q2 + e) * L::kMergePitch + r * (D / 8);
+      for (int w0 = 0; w0 < kWarps; w0 += kMergeWarps) {
+        if (w0 <= warp && warp < w0 + kMergeWarps) {
 #pragma unroll
-        for (int j = 0; j < kSteps; j += 2)
-          *reinterpret_cast<float4*>(at + 2 * j) =
-              make_float4(o[j][t][e] * f, o[j][t][e + 2] * f, o[j + 1][t][e] * f, o[j + 1][t][e + 2] * f);
+          for (int e = 0; e < 2; ++e) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sml[w * kRows + 8 * t + q2 + e].x);
+            const float f = m[t][e] == -INFINITY ? 0.0f : exp2_fast(m[t][e] - top) * vref;
+            float* at = merge + ((warp - w0) * 8 + q2 + e) * L::kMergePitch + r * (D / 8);
+#pragma unroll
+            for (int j = 0; j < kSteps; j += 2)
+              *reinterpret_cast<float4*>(at + 2 * j) =
+                  make_float4(o[j][t][e] * f, o[j][t][e + 2] * f, o[j + 1][t][e] * f, o[j + 1][t][e + 2] * f);
+          }
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
+#pragma unroll
+        for (int y = 0; y < kMine; ++y) {
+          const int x = threadIdx.x + y * kWarps * 32;
+          if (x < kParts) {
+            const float* at = merge + x / (D / 4) * L::kMergePitch + x % (D / 4) * 4;
+#pragma unroll
+            for (int w = w0; w < kWarps && w < w0 + kMergeWarps; ++w) {
+              const float4 v = *reinterpret_cast<const float4*>(at + (w - w0) * 8 * L::kMergePitch);
+              sums[y].x += v.x;
+              sums[y].y += v.y;
+              sums[y].z += v.z;
+              sums[y].w += v.w;
+            }
+          }
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
       }
-      asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-      for (int x = threadIdx.x; x < 8 * (D / 4); x += kWarps * 32) {
+#pragma unroll
+      for (int y = 0; y < kMine; ++y) {
+        const int x = threadIdx.x + y * kWarps * 32;
+        if (x >= kParts) continue;
+        const float4 sum = sums[y];
         const int qi = x / (D / 4), d = x % (D / 4) * 4, row = 8 * t + qi;
-        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         float top = -INFINITY, den = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sml[w * kRows + row].x);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          const float4 y = *reinterpret_cast<const float4*>(merge + (w * 8 + qi) * L::kMergePitch + d);
-          sum.x += y.x;
-          sum.y += y.y;
-          sum.z += y.z;
-          sum.w += y.w;
           const float2 ml = sml[w * kRows + row];
           den += ml.x == -INFINITY ? 0.0f : ml.y * exp2_fast(ml.x - top);
         }
@@ -634,8 +696,8 @@ __global__ void __launch_bounds__(kStreamThreads, 1)
           if (d == 0) s.part_ml[(size_t)slot * kRows + row] = make_float2(top, den);
         }
       }
-      asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
     }
+    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");     // sml is read no more
   }
 }
 
@@ -646,6 +708,7 @@ constexpr int kFinishKeys = 1024;
 // grid (parts of the slots, key heads * batch); the first part also joins the pieces
 template <int D>
 __global__ void __launch_bounds__(kFinishThreads) kv_finish_kernel(const KvView c, const StreamArgs s, int ctas, int row_slots) {
+  constexpr int kTile = tile_of(D);
   __shared__ float2 stat[kKvStreamMaxRows];       // maximum, 1 / sum of a row
   const int pair = blockIdx.y, b = pair / c.kv_heads, head = pair % c.kv_heads;
   const int len = seq_len(c, b), n = seq_queries(s.a, b), rows = n * s.a.group;
@@ -654,7 +717,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv_finish_kernel(const KvView 
   // tiles before this sequence: those of the sequences 0 .. b - 1
   int64_t before = 0, all = 0;
   for (int i = threadIdx.x; i < s.a.batch; i += kFinishThreads) {
-    const int64_t t = (int64_t)c.kv_heads * seq_key_tiles(c, s.a, i);
+    const int64_t t = (int64_t)c.kv_heads * seq_key_tiles<kTile>(c, s.a, i);
     all += t;
     if (i < b) before += t;
   }
@@ -669,7 +732,7 @@ __global__ void __launch_bounds__(kFinishThreads) kv_finish_kernel(const KvView 
   before = all = 0;
 #pragma unroll
   for (int w = 0; w < kFinishThreads / 32; ++w) { before += sums[w][0]; all += sums[w][1]; }
-  const int tiles = seq_key_tiles(c, s.a, b);
+  const int tiles = seq_key_tiles<kTile>(c, s.a, b);
   const int64_t line = before + (int64_t)head * tiles;
   const int working = working_ctas(all, ctas);
   const int c0 = tiles ? tile_owner(all, line, working) : 0, c1 = tiles ? tile_owner(all, line + tiles - 1, working) : 0;
@@ -757,14 +820,14 @@ int row_slots_of(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32); }
 
 struct Workspace { size_t part_o, part_ml, pair_ml, z, total; };
 Workspace plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d, bool weights) {
-  const int rows = d->tokens * (d->heads / c->kv_heads), slots = row_slots_of(rows);
-  const size_t tiles = (size_t)q->batch * c->kv_heads * ((spv_kv_max_length(c, q) + kTile - 1) / kTile);
+  const int rows = d->tokens * (d->heads / c->kv_heads), slots = row_slots_of(rows), tile = tile_of(c->head_dim);
+  const size_t tiles = (size_t)q->batch * c->kv_heads * ((spv_kv_max_length(c, q) + tile - 1) / tile);
   Workspace w;
   w.part_o = 0;
   w.part_ml = w.part_o + spv_align_up((size_t)kMaxCtas * kPartSlots * slots * c->head_dim * sizeof(float), 256);
   w.pair_ml = w.part_ml + spv_align_up((size_t)kMaxCtas * kPartSlots * slots * sizeof(float2), 256);
   w.z = w.pair_ml + spv_align_up((size_t)q->batch * c->kv_heads * slots * sizeof(float2), 256);
-  w.total = w.z + (weights ? spv_align_up(tiles * rows * kTile * sizeof(float), 256) : 0);
+  w.total = w.z + (weights ? spv_align_up(tiles * rows * tile * sizeof(float), 256) : 0);
   return w;
 }
 
@@ -773,13 +836,13 @@ int32_t launch(spv_ctx* ctx, int which, const CUtensorMap& mk, const CUtensorMap
                int ctas, cudaStream_t stream) {
   constexpr int bytes = Layout<D, NT>::kTotal + 1024;
   static_assert(bytes <= 227 * 1024, "shared memory");
-  static_assert(Layout<D, NT>::kStages >= 4, "too few stages");
+  static_assert(Layout<D, NT>::kOwn >= 2, "a warp works on one stage while another fills");
   auto kernel = kv_stream_kernel<FMT, D, NT>;
   if (!(ctx->kv_configured & (1u << which))) {
     SPV_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     ctx->kv_configured |= 1u << which;
   }
-  kernel<<<ctas, kStreamThreads, bytes, stream>>>(mk, mv, view, s);
+  kernel<<<ctas, Layout<D, NT>::kThreads, bytes, stream>>>(mk, mv, view, s);
   return cudaGetLastError() == cudaSuccess ? SPV_OK : SPV_ERR_CUDA;
 }
 
@@ -808,13 +871,14 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   const uint64_t lines = (uint64_t)cache->pages * cache->kv_heads * cache->block * cache->head_dim / 128;
   const uint64_t dims[2] = {128, lines};
   const uint64_t strides[1] = {128};
-  const uint32_t part = cache->block < kTile ? cache->block : kTile;
+  const int tile = tile_of(cache->head_dim);
+  const uint32_t part = cache->block < tile ? cache->block : tile;
   const uint32_t box[2] = {128, part * cache->head_dim / 128};
   CUtensorMap mk, mv;
   int32_t st = spv_make_tmap_u8(ctx, &mk, cache->k, 2, dims, strides, box);
   if (st != SPV_OK) return st;
   if ((st = spv_make_tmap_u8(ctx, &mv, cache->v, 2, dims, strides, box)) != SPV_OK) return st;
-  const int64_t most = (int64_t)seqs->batch * cache->kv_heads * ((view.max_length + kTile - 1) / kTile);
+  const int64_t most = (int64_t)seqs->batch * cache->kv_heads * ((view.max_length + tile - 1) / tile);
   int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
   if (most < ctas) ctas = (int)most;
   const int slots = row_slots_of(s.rows);

@@ -296,6 +296,14 @@ def test_attention_long(ctx, fmt, dtype, dim):
     run_attention(ctx, rng, [5003], 4, None, 12, 1, dim, 128, fmt, dtype, True, weights=False)
 
 
+@pytest.mark.parametrize("fmt,dtype,dim,group,tokens", [("int8", "bf16", 128, 1, 1), ("e4m3", "bf16", 64, 3, 4),
+                                                        ("e4m3", "fp16", 128, 4, 7)])
+def test_attention_many_tiles_for_every_sm(ctx, fmt, dtype, dim, group, tokens):
+    """Far more key tiles than the kernels hold at a time, in stretches that cross several sequences and heads."""
+    rng = np.random.default_rng(dim + group)
+    run_attention(ctx, rng, [9001, 40, 0, 7777, 3000, 1, 5000], tokens, None, 8 * group, 8, dim, 64, fmt, dtype, True)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_attention_uneven_scales(ctx, fmt):
     """Blocks whose keys and values differ by many powers of two, an all-zero block, one far larger than the rest."""
