@@ -141,6 +141,8 @@ int32_t check_attn(const spv_kv_cache* c, const spv_kv_seqs* s, const spv_kv_att
   if (d->causal != 0 && d->causal != 1) return SPV_ERR_INVALID_ARG;
   if (!(d->softmax_scale >= 0.0f) || d->softmax_scale > 1e30f) return SPV_ERR_INVALID_ARG;
   if ((int64_t)d->tokens * d->heads > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
+  // tiles of 32 slots are numbered in 31 bits
+  if ((int64_t)s->batch * c->kv_heads * ((spv_kv_max_length(c, s) + 31) / 32) > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
   const int64_t strides[6] = {d->q_stride_b, d->q_stride_tok, d->q_stride_head, d->o_stride_b, d->o_stride_tok, d->o_stride_head};
   for (int64_t x : strides)
     if (x % 8) return SPV_ERR_ALIGNMENT;

@@ -2,17 +2,18 @@
 //
 // Bound by HBM: 2 * head_dim bytes a key and key head are read once, for 4 * head_dim * rows operations.
 //
-//   kv_stream_kernel  one CTA per SM.  All key tiles (8 KB) of all (sequence, key head) pairs form one line,
-//                     and every CTA takes an equal stretch of it, whatever the lengths are.  A producer warp brings
-//                     the tiles in by TMA (as many in flight as shared memory holds: the latency of HBM times its
-//                     rate is 35 KB an SM); the other warps take them in turn, each with an online softmax of its own,
-//                     and join their states where the pair changes.  Codes go from shared memory to fp16 fragments
-//                     in registers (the 128-byte swizzle makes the 16-byte reads of both operands free of bank
-//                     conflicts), and the products run with keys as the rows: S^T = K Q^T and O^T = V^T P^T, so
-//                     that eight queries fill the narrow side of mma.m16n8k16 and P^T comes out of the score
-//                     fragments with one 8 x 8 transpose.
-//   kv_finish_kernel  joins the pieces of pairs that were cut between CTAs, and turns the stored scores into
-//                     attention weights.
+//   kv_stream_kernel  one CTA per SM.  All key tiles (8 KB) of all (sequence, key head) pairs form one line, and every
+//                     warp takes an equal stretch of it, whatever the lengths are, with nothing to wait for in other
+//                     warps: it brings its tiles in by TMA into stages of its own, refills a stage as soon as it has
+//                     used it, and keeps queries, maxima, sums and results of the pair it is at in registers.  (With
+//                     stretches per CTA the warps had to join at every change of pair: of 24 sequences of 400 to 8191
+//                     slots the CTAs with the short ones took twice as long as the others.)
+//                     Codes go from shared memory to fp16 fragments in registers (the 128-byte swizzle makes the
+//                     16-byte reads of both operands free of bank conflicts), and the products run with keys as the
+//                     rows: S^T = K Q^T and O^T = V^T P^T, so that eight queries fill the narrow side of mma.m16n8k16
+//                     and P^T comes out of the score fragments with one 8 x 8 transpose.
+//   kv_finish_kernel  joins the pieces of pairs that were cut between warps, and turns the stored scores into attention
+//                     weights; its blocks take equal stretches of the same line.
 //
 // Numbers: queries are scaled by a power of two of their own (largest magnitude in [2^14, 2^15)) into fp16, exactly but
 // for elements below 2^-28 of their row's largest; codes are exact in fp16; sums are fp32.  Probabilities are rounded to
@@ -26,17 +27,22 @@ using namespace spv;
 
 // slots of a key tile: 8 KB of keys and values
 __host__ __device__ constexpr int tile_of(int head_dim) { return head_dim == 128 ? 32 : 64; }
-constexpr int kMergeWarps = 8;               // warps whose results are added up at a time
-constexpr int kPartSlots = 2;                // pieces a CTA can leave: of the pair it began in, of the one it ended in
+constexpr int kPartSlots = 2;                // pieces a worker can leave: of the pair it began in, of the one it ended in
 constexpr float kLazy = 8.0f;
-constexpr int kIssue = 4;                    // tiles that the producer's lanes bring in side by side
+
+// The first piece of a worker's stretch, for the second kernel.
+struct alignas(16) Stretch {
+  int total, before;                       // tiles in all, and before sequence b
+  int b, head, len, n, tiles, kt0;
+};
 
 struct StreamArgs {
   KvAttnArgs a;
   float* z;             // scores (log2 domain) [tile][rows][slot], NULL when no weights are wanted
-  float* part_o;        // [CTA][2][8 NT][D] unnormalised
-  float2* part_ml;      // [CTA][2][8 NT] maximum, sum
-  float2* pair_ml;      // [pair][8 NT]: the same of pairs that one CTA had whole
+  float* part_o;        // [worker][2][8 NT][D] unnormalised
+  float2* part_ml;      // [8 NT][2][worker] maximum, sum: a row's pieces side by side
+  float2* pair_ml;      // [pair][8 NT]: the same of pairs that one worker had whole
+  Stretch* stretch;     // [worker]
   int32_t rows;         // tokens * group
 };
 
@@ -46,43 +52,35 @@ struct StageMeta {      // of one tile, by 16-slot quarters
   int pad[3];
 };
 
+__host__ __device__ constexpr int warps_of(int row_slots) { return row_slots == 8 ? 12 : 8; }   // 168 or 255 registers
+
 template <int D, int NT>
 struct Layout {
-  // place of tile `it` of the CTA, and the phase of that stage's barriers
-  __device__ static int stage(uint32_t it) { return (int)(it % kWarps * kOwn + it / kWarps % kOwn); }
-  __device__ static uint32_t phase(uint32_t it) { return it / kWarps / kOwn; }
   static constexpr int kTile = tile_of(D);
-  // consumer warps: with the producer 3 or 2 a scheduler, which leaves 168 or 255 registers a thread
-  static constexpr int kWarps = NT < 4 ? 11 : 7;
-  static constexpr int kThreads = (kWarps + 1) * 32;
+  static constexpr int kWarps = warps_of(8 * NT);
+  static constexpr int kThreads = kWarps * 32;
   static constexpr int kStageBytes = 2 * kTile * D;
-  static constexpr int kMergePitch = D + 4;
-  static constexpr int kMerge = kMergeWarps * 8 * kMergePitch * 4;
-  static constexpr int kQ = NT * (D / 16) * 32 * 8;
-  static constexpr int kRows = 8 * NT;
-  static constexpr int kSmall = kRows * 4 * 2 + kWarps * kRows * 8 + 2048;
+  static constexpr int kQ = NT == 4 ? kWarps * NT * (D / 16) * 32 * 8 : 0;     // queries that registers do not hold
   static constexpr int kBudget = 227 * 1024 - 1024;
-  static constexpr int kFit = (kBudget - kMerge - kQ - kSmall) / (kStageBytes + (int)sizeof(StageMeta) + 16);
-  // Stages belong to one consumer warp each, which waits for their phases one after the other: a parity says which of
-  // two phases is over, so nobody may wait for a phase while the one before it is still to come.
+  static constexpr int kFit = (kBudget - kQ - 1024) / (kStageBytes + (int)sizeof(StageMeta) + 8);
+  // Stages belong to one warp each, which waits for their phases one after the other: a parity says which of two
+  // phases is over, so nobody may wait for a phase while the one before it is still to come.
   static constexpr int kOwn = kFit / kWarps;
   static constexpr int kStages = kOwn * kWarps;
-  static constexpr int oMerge = kStages * kStageBytes;
-  static constexpr int oQ = oMerge + kMerge;
+  static constexpr int oQ = kStages * kStageBytes;
   static constexpr int oMeta = oQ + kQ;
   static constexpr int oBars = oMeta + kStages * (int)sizeof(StageMeta);
-  static constexpr int oEnd = oBars + kStages * 16;
-  static constexpr int oFactor = oEnd + kRows * 4;
-  static constexpr int oMl = oFactor + kRows * 4;                       // float2 [warp][row]
-  static constexpr int oScan = oMl + kWarps * kRows * 8;
+  static constexpr int oScan = oBars + kStages * 8;
   static constexpr int kTotal = oScan + 512;
 };
 
 // ---- the line of tiles -------------------------------------------------------------------------
+// Places on the line are 32-bit (the host refuses longer lines): a 64-bit division costs hundreds of cycles, and both
+// kernels begin with several.
 struct Scan {
-  int64_t total, before;     // tiles of all sequences; of those before the one that holds the target
-  int64_t warp_sum[16];
-  int b;
+  int total;                 // tiles of all sequences
+  int warp_sum[16];
+  int b[16], before[16];     // of each warp's worker: the sequence its stretch begins in, the tiles before that
 };
 
 __device__ __forceinline__ int seq_len(const KvView& c, int b) { return spv_kv_clamp(__ldg(c.lengths + b), c.max_length); }
@@ -94,76 +92,88 @@ __device__ __forceinline__ int seq_key_tiles(const KvView& c, const KvAttnArgs& 
   return seq_queries(a, b) > 0 ? (seq_len(c, b) + TILE - 1) / TILE : 0;
 }
 
-// Sums the tiles of all sequences; then the sequence that holds tile `share(total)`.  All threads of the CTA.
+// Equal stretches of the line: the first `more` workers have per + 1 tiles, the others per.  Only as many work as there
+// are tiles: every one has a tile at least, so that no piece between two others is missing.
+struct Share {
+  int working, per, more;
+  __device__ __forceinline__ Share(int total, int workers) {
+    working = min(total, workers);
+    per = working ? total / working : 0;
+    more = working ? total % working : 0;
+  }
+  __device__ __forceinline__ int begin(int worker) const { return worker * per + min(worker, more); }
+  __device__ __forceinline__ int owner(int t) const {
+    const int wide = more * (per + 1);
+    return t < wide ? t / (per + 1) : more + (t - wide) / per;
+  }
+};
+
+// Sums the tiles of all sequences; then, for each warp, the sequence that holds tile `first(total, warp)`.  All threads.
 template <int THREADS, int TILE, typename F>
-__device__ __forceinline__ void scan_tiles(const KvView& c, const KvAttnArgs& a, Scan* s, F share) {
+__device__ __forceinline__ void scan_tiles(const KvView& c, const KvAttnArgs& a, Scan* s, F first) {
   const int per = (a.batch + THREADS - 1) / THREADS;
   const int b0 = threadIdx.x * per, b1 = min(a.batch, b0 + per);
-  int64_t sum = 0;
-  for (int b = b0; b < b1; ++b) sum += (int64_t)c.kv_heads * seq_key_tiles<TILE>(c, a, b);
-  int64_t inc = sum;
+  int sum = 0;
+  for (int b = b0; b < b1; ++b) sum += c.kv_heads * seq_key_tiles<TILE>(c, a, b);
+  int inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, inc, o);
+    const int x = __shfl_up_sync(0xffffffffu, inc, o);
     if ((threadIdx.x & 31) >= o) inc += x;
   }
   if ((threadIdx.x & 31) == 31) s->warp_sum[threadIdx.x >> 5] = inc;
   __syncthreads();
-  int64_t base = 0, total = 0;
+  int base = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
     if (w < (threadIdx.x >> 5)) base += s->warp_sum[w];
     total += s->warp_sum[w];
   }
-  const int64_t target = share(total);
-  int64_t at = base + inc - sum;
-  if (target >= at && target < at + sum) {
-    int b = b0;
-    for (;; ++b) {
-      const int64_t t = (int64_t)c.kv_heads * seq_key_tiles<TILE>(c, a, b);
-      if (target < at + t || b + 1 >= b1) break;
-      at += t;
+  const int at0 = base + inc - sum;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const int target = first(total, w);
+    int at = at0;
+    if (target >= at && target < at + sum) {
+      int b = b0;
+      for (;; ++b) {
+        const int t = c.kv_heads * seq_key_tiles<TILE>(c, a, b);
+        if (target < at + t || b + 1 >= b1) break;
+        at += t;
+      }
+      s->b[w] = b;
+      s->before[w] = at;
     }
-    s->b = b;
-    s->before = at;
   }
   if (threadIdx.x == 0) s->total = total;
   __syncthreads();
 }
 
-// CTAs that get a stretch: every one of them has a tile at least, so that no piece between two others is missing.
-__device__ __forceinline__ int working_ctas(int64_t total, int ctas) { return (int)min(total, (int64_t)ctas); }
-__device__ __forceinline__ int64_t stretch_begin(int64_t total, int cta, int ctas) { return total * cta / ctas; }
-// the CTA whose stretch holds tile t
-__device__ __forceinline__ int tile_owner(int64_t total, int64_t t, int ctas) { return (int)(((t + 1) * ctas - 1) / total); }
-
 // One piece of a pair: key tiles [kt0, kt1) of `tiles`.
 struct Piece {
   int b, head, len, n, tiles, kt0, kt1;
-  int64_t line;              // place of kt0 on the line
+  int line;                  // place of the pair's first tile on the line
 };
 struct Walk {
-  int64_t pos, end, before;
-  int b;
+  int pos, end, before, b;
 };
 template <int TILE>
 __device__ __forceinline__ bool next_piece(const KvView& c, const KvAttnArgs& a, Walk& w, Piece& p) {
   if (w.pos >= w.end) return false;
   int tiles = seq_key_tiles<TILE>(c, a, w.b);
-  while (w.pos >= w.before + (int64_t)c.kv_heads * tiles) {
-    w.before += (int64_t)c.kv_heads * tiles;
+  while (w.pos >= w.before + c.kv_heads * tiles) {
+    w.before += c.kv_heads * tiles;
     if (++w.b >= a.batch) return false;
     tiles = seq_key_tiles<TILE>(c, a, w.b);
   }
-  const int off = (int)(w.pos - w.before);
+  const int off = w.pos - w.before;
   p.b = w.b;
   p.head = off / tiles;
   p.kt0 = off % tiles;
-  p.kt1 = (int)min((int64_t)tiles, p.kt0 + (w.end - w.pos));
+  p.kt1 = min(tiles, p.kt0 + (w.end - w.pos));
   p.tiles = tiles;
   p.len = seq_len(c, w.b);
   p.n = seq_queries(a, w.b);
-  p.line = w.pos;
+  p.line = w.pos - p.kt0;
   w.pos += p.kt1 - p.kt0;
   return true;
 }
@@ -187,48 +197,45 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
   return v;
 }
 
-// Queries of a pair to shared memory in fragment order: [query tile][k step][lane][4], lane = 4 * query + c, the four
-// values d = (D/4) c + 4 step .. + 3.  Rows behind the last are zeros.
-template <int D, int NT>
-__device__ __forceinline__ void load_queries(const StreamArgs& s, const Piece& p, uint16_t* q, float* factor, int* ends) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kPer = D / 32;     // elements of a row for each lane
-  for (int row = warp; row < 8 * NT; row += Layout<D, NT>::kWarps) {
-    const int i = row / s.a.group, head = p.head * s.a.group + row % s.a.group;
-    float x[kPer];
+// Queries 8t .. 8t + 7 of a pair as fragments: lane 4q + c gets the D / 4 values d = (D/4) c .. of query q, scaled by a
+// power of two of the row's own.  Returns the exponent that the row was scaled down by; rows behind the last are zeros.
+template <int D>
+__device__ __forceinline__ int load_queries(const StreamArgs& s, const Piece& p, int t, uint2* f) {
+  const int lane = threadIdx.x & 31, row = 8 * t + (lane >> 2), c = lane & 3;
+  const int i = row / s.a.group, head = p.head * s.a.group + row % s.a.group;
+  uint4 w[D / 32];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) x[e] = 0.0f;
-    const bool real = i < p.n;
-    if (real) {
-      const uint16_t* src = s.a.q + p.b * s.a.q_stride_b + i * s.a.q_stride_tok + head * s.a.q_stride_head + lane * kPer;
-      uint32_t w[kPer / 2];
+  for (int x = 0; x < D / 32; ++x) w[x] = make_uint4(0u, 0u, 0u, 0u);
+  if (i < p.n) {
+    const uint16_t* src = s.a.q + p.b * s.a.q_stride_b + i * s.a.q_stride_tok + head * s.a.q_stride_head + c * (D / 4);
 #pragma unroll
-      for (int e = 0; e < kPer / 2; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
+    for (int x = 0; x < D / 32; ++x) w[x] = __ldg(reinterpret_cast<const uint4*>(src) + x);
+  }
+  auto value = [&](uint32_t u) { return s.a.dtype == SPV_BF16 ? kv_unpack2<SPV_BF16>(u) : kv_unpack2<SPV_FP16>(u); };
+  uint32_t big = 0;
 #pragma unroll
-      for (int e = 0; e < kPer / 2; ++e) {
-        const float2 f = s.a.dtype == SPV_BF16 ? kv_unpack2<SPV_BF16>(w[e]) : kv_unpack2<SPV_FP16>(w[e]);
-        x[2 * e] = f.x;
-        x[2 * e + 1] = f.y;
-      }
-    }
-    uint32_t big = 0;
+  for (int x = 0; x < D / 32; ++x) {
+    const uint32_t u[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) big = max(big, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-    big = __reduce_max_sync(0xffffffffu, big);
-    const int ex = max((int)(big >> 23) - 127, -100);
-    const float up = kv_pow2(14 - ex);
-#pragma unroll
-    for (int e = 0; e < kPer; e += 2) {
-      const __half2 h = __floats2half2_rn(x[e] * up, x[e + 1] * up);
-      const int d = lane * kPer + e, c = d / (D / 4), step = d % (D / 4) / 4;
-      const int at = (((row >> 3) * (D / 16) + step) * 32 + (row & 7) * 4 + c) * 4 + (d & 3);
-      *reinterpret_cast<__half2*>(q + at) = h;
-    }
-    if (lane == 0) {
-      factor[row] = s.a.scale * 1.4426950408889634f * kv_pow2(ex - 14);
-      ends[row] = real ? spv_kv_query_end(p.len, p.n, i, s.a.causal) : p.len;
+    for (int y = 0; y < 4; ++y) {
+      const float2 v = value(u[y]);
+      big = max(big, max(__float_as_uint(v.x) & 0x7FFFFFFFu, __float_as_uint(v.y) & 0x7FFFFFFFu));
     }
   }
+  big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+  big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+  const int ex = max((int)(big >> 23) - 127, -100);
+  const float up = kv_pow2(14 - ex);
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x) {
+    const uint32_t u[4] = {w[x].x, w[x].y, w[x].z, w[x].w};
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const float2 v0 = value(u[2 * y]), v1 = value(u[2 * y + 1]);
+      f[2 * x + y] = make_uint2(kv_pack2<SPV_FP16>(v0.x * up, v0.y * up), kv_pack2<SPV_FP16>(v1.x * up, v1.y * up));
+    }
+  }
+  return ex - 14;
 }
 
 template <int FMT, int D, int NT>
@@ -236,7 +243,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
     kv_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const KvView c,
                      const StreamArgs s) {
   using L = Layout<D, NT>;
-  constexpr int kRows = L::kRows;
+  constexpr int kRows = 8 * NT;
   constexpr int kWarps = L::kWarps;
   constexpr int kTile = L::kTile;
   constexpr int kQuarters = kTile / 16;        // scales are kept for 16 slots each
@@ -245,14 +252,8 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
   constexpr int kMt = kKeys / 16;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-  float* merge = reinterpret_cast<float*>(smem + L::oMerge);
-  uint16_t* sq = reinterpret_cast<uint16_t*>(smem + L::oQ);
   StageMeta* meta = reinterpret_cast<StageMeta*>(smem + L::oMeta);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::oBars);
-  uint64_t* empty = full + L::kStages;
-  int* ends = reinterpret_cast<int*>(smem + L::oEnd);
-  float* factor = reinterpret_cast<float*>(smem + L::oFactor);
-  float2* sml = reinterpret_cast<float2*>(smem + L::oMl);
   Scan* scan = reinterpret_cast<Scan*>(smem + L::oScan);
   volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + L::oScan + 256);
   uint32_t* wait_status = c.status - 1;
@@ -261,10 +262,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
-    for (int i = 0; i < L::kStages; ++i) {
-      mbar_init(full + i, 2);
-      mbar_init(empty + i, 1);
-    }
+    for (int i = 0; i < L::kStages; ++i) mbar_init(full + i, 1);
     mbar_fence_init();
     *abort_flag = 0u;
   }
@@ -274,140 +272,130 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
       if (s.a.counts) kv_clamped(__ldg(s.a.counts + b), s.a.tokens, c.status);
     }
   }
-  scan_tiles<L::kThreads, kTile>(c, s.a, scan, [&](int64_t total) {
-    const int w = working_ctas(total, gridDim.x);
-    return blockIdx.x < w ? stretch_begin(total, blockIdx.x, w) : total;
+  // neighbours on the line are on different SMs, so that few tiles are spread over all of them
+  const int workers = gridDim.x * kWarps, worker = warp * gridDim.x + blockIdx.x;
+  scan_tiles<L::kThreads, kTile>(c, s.a, scan, [&](int total, int w) {
+    const Share share(total, workers);
+    const int at = w * gridDim.x + blockIdx.x;
+    return at < share.working ? share.begin(at) : total;
   });
+  const Share share(scan->total, workers);
   asm volatile("griddepcontrol.launch_dependents;");
-  const int64_t total = scan->total;
-  const int working = working_ctas(total, gridDim.x);
-  if (blockIdx.x >= working) return;
   Walk walk;
-  walk.pos = stretch_begin(total, blockIdx.x, working);
-  walk.end = stretch_begin(total, blockIdx.x + 1, working);
-  walk.before = scan->before;
-  walk.b = scan->b;
-  Piece p;
-
-  if (warp == kWarps) {
-    // ---- producer: every lane has a tile of its own, and kIssue lanes at a time wait, copy and describe; the page
-    // numbers of the next 32 tiles are on their way meanwhile
-    uint64_t policy;
-    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
-    const int part = min(s.a.block, kTile);              // slots that one copy brings
-    const int parts = kTile / part;                      // copies of a tile: 1, 2 or 4
-    uint32_t it = 0;
-    while (next_piece<kTile>(c, s.a, walk, p)) {
-      const int32_t* row = c.table + p.b * c.table_stride;
-      int next[kQuarters];
-      auto fetch = [&](int kt) {
-#pragma unroll
-        for (int x = 0; x < kQuarters; ++x) {
-          const int slot = kt * kTile + x * part;
-          next[x] = x < parts && kt < p.kt1 && slot < p.len ? __ldg(row + slot / s.a.block) : INT32_MIN;
-        }
-      };
-      fetch(p.kt0 + lane);
-      for (int base = p.kt0; base < p.kt1; base += 32) {
-        const int kt = base + lane;
-        int page[kQuarters];
-        float ks[kQuarters], vs[kQuarters];
-        int loads = 0, bad = 0;
-#pragma unroll
-        for (int x = 0; x < kQuarters; ++x) {
-          page[x] = next[x];
-          ks[x] = vs[x] = 0.0f;                          // of parts that hold nothing
-          if (spv_kv_valid_page(page[x], c.pages)) {
-            const size_t ph = (size_t)page[x] * c.kv_heads + p.head;
-            ks[x] = __ldg(c.k_scale + ph);
-            vs[x] = __ldg(c.v_scale + ph);
-            ++loads;
-          } else if (x < parts && kt < p.kt1 && kt * kTile + x * part < p.len) {
-            kv_fault(c.status, SPV_SITE_KV_PAGE);
-            bad |= ((1 << kQuarters / parts) - 1) << x * (kQuarters / parts);
-          }
-        }
-        if (base + 32 < p.kt1) fetch(base + 32 + lane);
-        const int count = min(32, p.kt1 - base);
-        for (int j = 0; j < count; j += kIssue) {
-          if (lane >= j && lane < min(j + kIssue, count)) {
-            const uint32_t at = it + lane;
-            const int st = L::stage(at);
-            if (at >= L::kStages) mbar_wait(empty + st, (L::phase(at) - 1) & 1, abort_flag, wait_status, 0x4B01u);
-            uint8_t* kdst = smem + st * L::kStageBytes;
-            mbar_expect_tx(full + st, loads * 2 * part * D);
-#pragma unroll
-            for (int x = 0; x < kQuarters; ++x) {
-              if (spv_kv_valid_page(page[x], c.pages)) {
-                const int at_row = (int)(spv_kv_row(page[x], c.kv_heads, p.head, s.a.block, kt * kTile + x * part) / (128 / D));
-                tma_load_rows(kdst + x * part * D, &map_k, full + st, at_row, policy);
-                tma_load_rows(kdst + kTile * D + x * part * D, &map_v, full + st, at_row, policy);
-              }
-            }
-            StageMeta* m = meta + st;
-#pragma unroll
-            for (int x = 0; x < kQuarters; ++x) {
-              const int y = x * parts / kQuarters;       // part that quarter x is in
-              float kx = ks[0], vx = vs[0];
-#pragma unroll
-              for (int i = 1; i < kQuarters; ++i) {
-                kx = y == i ? ks[i] : kx;
-                vx = y == i ? vs[i] : vx;
-              }
-              m->ks[x] = kx;
-              m->vs[x] = vx;
-            }
-            m->bad = bad;
-            mbar_arrive(full + st);
-          }
-          __syncwarp();
-        }
-        it += count;
-      }
-    }
-    // nothing of this CTA is in flight when it ends: a wait that gave up leaves copies behind
-    if (*abort_flag != 0u && lane == 0) {
-      for (uint32_t i = it > L::kStages ? it - L::kStages : 0; i < it; ++i)
-        for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(full + L::stage(i), L::phase(i) & 1, 1000u); ++tries) {
-        }
-    }
+  walk.before = scan->before[warp];
+  walk.b = scan->b[warp];
+  if (worker >= share.working) {
+    if (lane == 0) s.stretch[worker].total = scan->total;
     return;
   }
+  walk.pos = share.begin(worker);
+  walk.end = share.begin(worker + 1);
+  Piece p;
 
-  // ---- consumers
+  // ---- what this warp brings in: tiles of its stretch, kOwn ahead of the one it works on
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  const int part = min(s.a.block, kTile);              // slots that one copy brings
+  const int parts = kTile / part;                      // copies of a tile: 1, 2 or 4
+  const int stretch = walk.end - walk.pos;
+  Walk fwalk = walk;
+  Piece fp;
+  int f_begin = 0, f_end = 0, f_batch = -1;            // tiles of the piece being fed; first tile of the lanes' batch
+  int f_row = -1, f_lost = 0;                          // this lane's copy: line of the pool, or none
+  float f_ks = 0.0f, f_vs = 0.0f;
+  // tile `it` of the stretch into stage `st`; the lanes know the pages of the next 32 / parts tiles
+  auto feed = [&](int it, int st) {
+    if (it >= stretch) return;
+    while (it >= f_end) {
+      next_piece<kTile>(c, s.a, fwalk, fp);
+      f_begin = f_end;
+      f_end += fp.kt1 - fp.kt0;
+      f_batch = -1;
+    }
+    int at = f_batch < 0 ? 32 : (it - f_batch) * parts;
+    if (at >= 32) {
+      f_batch = it;
+      at = 0;
+      const int mine = it + lane / parts, slot = (fp.kt0 + mine - f_begin) * kTile + lane % parts * part;
+      f_row = -1;
+      f_lost = 0;
+      f_ks = f_vs = 0.0f;                              // of parts that hold nothing
+      if (mine < f_end && slot < fp.len) {
+        const int page = kv_page(c.table + fp.b * c.table_stride, slot / s.a.block, c.pages, c.status);
+        if (page >= 0) {
+          const size_t ph = (size_t)page * c.kv_heads + fp.head;
+          f_ks = __ldg(c.k_scale + ph);
+          f_vs = __ldg(c.v_scale + ph);
+          f_row = (int)(spv_kv_row(page, c.kv_heads, fp.head, s.a.block, slot) / (128 / D));
+        } else {
+          f_lost = 1;
+        }
+      }
+    }
+    const bool mine = lane >= at && lane < at + parts;
+    const int loads = __popc(__ballot_sync(0xffffffffu, mine && f_row >= 0));
+    const uint32_t lost = __ballot_sync(0xffffffffu, mine && f_lost) >> at;
+    if (lane == at) {
+      mbar_expect_tx(full + st, loads * 2 * part * D);
+      int bad = 0;
+#pragma unroll
+      for (int x = 0; x < kQuarters; ++x) bad |= (int)(lost >> (x * parts / kQuarters) & 1u) << x;
+      meta[st].bad = bad;
+    }
+    __syncwarp();
+    if (mine) {
+      const int x0 = lane - at;
+      if (f_row >= 0) {
+        uint8_t* dst = smem + st * L::kStageBytes + x0 * part * D;
+        tma_load_rows(dst, &map_k, full + st, f_row, policy);
+        tma_load_rows(dst + kTile * D, &map_v, full + st, f_row, policy);
+      }
+      for (int x = x0 * kQuarters / parts; x < (x0 + 1) * kQuarters / parts; ++x) {
+        meta[st].ks[x] = f_ks;
+        meta[st].vs[x] = f_vs;
+      }
+    }
+    __syncwarp();
+  };
+  const int own = warp * L::kOwn;
+#pragma unroll
+  for (int i = 0; i < L::kOwn; ++i) feed(i, own + i);
+  int slot_at = 0;             // which of its stages is next, and the phase of its barrier
+  uint32_t phase = 0;
+
   const int r = lane >> 2, q2 = (lane & 3) * 2;
-  uint32_t ring = 0;
+  int it = 0;                  // tile of the stretch
   while (next_piece<kTile>(c, s.a, walk, p)) {
-    load_queries<D, NT>(s, p, sq, factor, ends);
-    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-    const int full_end = ends[0];           // slots that every query sees (row 0 sees least)
+    if (it == 0 && lane == 0) s.stretch[worker] = Stretch{scan->total, walk.before, p.b, p.head, p.len, p.n, p.tiles, p.kt0};
+    const int full_end = spv_kv_query_end(p.len, p.n, 0, s.a.causal);     // slots that every query sees (the first sees least)
     float o[kSteps][NT][4];
     float m[NT][2], l[NT][2], qf[NT][2];
     float vref = 0.0f, vtop = 0.0f;         // unit of o; largest value scale met
+    uint2 qr[NT == 4 ? 1 : NT][NT == 4 ? 1 : kSteps];
+    const uint32_t sq_at = smem_u32(smem) + L::oQ + warp * (L::kQ / kWarps) + lane * 8;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
+      uint2 f[kSteps];
+      const int ex = load_queries<D>(s, p, t, f);
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        if (NT == 4) asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(sq_at + (t * kSteps + j) * 256), "r"(f[j].x), "r"(f[j].y) : "memory");
+        else qr[NT == 4 ? 0 : t][NT == 4 ? 0 : j] = f[j];
+      }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         m[t][e] = -INFINITY;
         l[t][e] = 0.0f;
-        qf[t][e] = factor[8 * t + q2 + e];
+        qf[t][e] = s.a.scale * 1.4426950408889634f * kv_pow2(__shfl_sync(0xffffffffu, ex, (q2 + e) * 4));
       }
 #pragma unroll
       for (int j = 0; j < kSteps; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[j][t][e] = 0.0f;
     }
-    uint2 qr[NT == 1 ? kSteps : 1];
-    const uint32_t sq_at = smem_u32(sq) + lane * 8;
-    if (NT == 1) {
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) qr[NT == 1 ? j : 0] = lds64(sq_at + j * 256);
-    }
-    const uint32_t ring_end = ring + (p.kt1 - p.kt0);
-    for (uint32_t it = ring + (warp + kWarps - ring % kWarps) % kWarps; it < ring_end; it += kWarps) {
-      const int st = L::stage(it);
-      const int kt = p.kt0 + (int)(it - ring);
-      mbar_wait(full + st, L::phase(it) & 1, abort_flag, wait_status, 0x4B02u);
+    for (int kt = p.kt0; kt < p.kt1; ++kt, ++it) {
+      const int st = own + slot_at;
+      mbar_wait(full + st, phase, abort_flag, wait_status, 0x4B02u);
       const uint32_t kbase = smem_u32(smem) + st * L::kStageBytes, vbase = kbase + kTile * D;
       const StageMeta* mt_at = meta + st;
       const int bad = mt_at->bad;
@@ -459,7 +447,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
             kv_half4<FMT>(wb[j], a1, a3);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-              const uint2 b = NT == 1 ? qr[NT == 1 ? j : 0] : lds64(sq_at + (t * kSteps + j) * 256);
+              const uint2 b = NT == 4 ? lds64(sq_at + (t * kSteps + j) * 256) : qr[NT == 4 ? 0 : t][NT == 4 ? 0 : j];
               mma_16816(z[i][t], a0, a1, a2, a3, b.x, b.y);
             }
           }
@@ -481,12 +469,16 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (slot + (e >> 1) * 8 >= ends[8 * t + q2 + (e & 1)] || (bad >> quarter & 1)) z[i][t][e] = -INFINITY;
+              for (int e = 0; e < 2; ++e) {
+                const int query = (8 * t + q2 + e) / s.a.group;
+                const int end = query < p.n ? spv_kv_query_end(p.len, p.n, query, s.a.causal) : p.len;
+                if (slot >= end || (bad >> quarter & 1)) z[i][t][e] = -INFINITY;
+                if (slot + 8 >= end || (bad >> quarter & 1)) z[i][t][e + 2] = -INFINITY;
+              }
           }
         }
         if (s.z) {
-          float* zt = s.z + (size_t)(p.line + (kt - p.kt0)) * s.rows * kTile;
+          float* zt = s.z + (size_t)(p.line + kt) * s.rows * kTile;
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -598,235 +590,259 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
           }
         }
       }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(empty + st);
+      __syncwarp();            // every lane has read the stage
+      feed(it + L::kOwn, st);
+      if (++slot_at == L::kOwn) {
+        slot_at = 0;
+        phase ^= 1u;
+      }
     }
-    ring = ring_end;
 
-    // ---- the warps' states into one
+    // ---- results of the piece: the pair's, or a part of them
+    const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
+    const int which = p.kt0 > 0 ? 0 : 1;
+    const size_t slot = (size_t)(2 * worker + which) * kRows;
+    const size_t pair = (size_t)(p.b * c.kv_heads + p.head) * kRows;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
         for (int sh = 4; sh < 32; sh <<= 1) l[t][e] += __shfl_xor_sync(0xffffffffu, l[t][e], sh);
-        if (r == 0) sml[warp * kRows + 8 * t + q2 + e] = make_float2(m[t][e], l[t][e]);
-      }
-    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-    const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
-    const int slot = 2 * blockIdx.x + (p.kt0 > 0 ? 0 : 1);
+        const int row = 8 * t + q2 + e;
+        constexpr int kMine = D / 8;                  // this thread's part of a row: d = kMine r ..
+        if (!whole) {
+          float* at = s.part_o + (slot + row) * D + r * kMine;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      constexpr int kParts = 8 * (D / 4);                              // float4s of eight queries' rows
-      constexpr int kMine = (kParts + kWarps * 32 - 1) / (kWarps * 32);
-      float4 sums[kMine];
-#pragma unroll
-      for (int y = 0; y < kMine; ++y) sums[y] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-      for (int w0 = 0; w0 < kWarps; w0 += kMergeWarps) {
-        if (w0 <= warp && warp < w0 + kMergeWarps) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sml[w * kRows + 8 * t + q2 + e].x);
-            const float f = m[t][e] == -INFINITY ? 0.0f : exp2_fast(m[t][e] - top) * vref;
-            float* at = merge + ((warp - w0) * 8 + q2 + e) * L::kMergePitch + r * (D / 8);
-#pragma unroll
-            for (int j = 0; j < kSteps; j += 2)
-              *reinterpret_cast<float4*>(at + 2 * j) =
-                  make_float4(o[j][t][e] * f, o[j][t][e + 2] * f, o[j + 1][t][e] * f, o[j + 1][t][e + 2] * f);
-          }
-        }
-        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-#pragma unroll
-        for (int y = 0; y < kMine; ++y) {
-          const int x = threadIdx.x + y * kWarps * 32;
-          if (x < kParts) {
-            const float* at = merge + x / (D / 4) * L::kMergePitch + x % (D / 4) * 4;
-#pragma unroll
-            for (int w = w0; w < kWarps && w < w0 + kMergeWarps; ++w) {
-              const float4 v = *reinterpret_cast<const float4*>(at + (w - w0) * 8 * L::kMergePitch);
-              sums[y].x += v.x;
-              sums[y].y += v.y;
-              sums[y].z += v.z;
-              sums[y].w += v.w;
-            }
-          }
-        }
-        asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");
-      }
-#pragma unroll
-      for (int y = 0; y < kMine; ++y) {
-        const int x = threadIdx.x + y * kWarps * 32;
-        if (x >= kParts) continue;
-        const float4 sum = sums[y];
-        const int qi = x / (D / 4), d = x % (D / 4) * 4, row = 8 * t + qi;
-        float top = -INFINITY, den = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sml[w * kRows + row].x);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float2 ml = sml[w * kRows + row];
-          den += ml.x == -INFINITY ? 0.0f : ml.y * exp2_fast(ml.x - top);
-        }
-        if (whole) {
+          for (int j = 0; j < kSteps; j += 2)
+            *reinterpret_cast<float4*>(at + 2 * j) = make_float4(o[j][t][e] * vref, o[j][t][e + 2] * vref,
+                                                                 o[j + 1][t][e] * vref, o[j + 1][t][e + 2] * vref);
+          if (r == 0) s.part_ml[(size_t)(2 * row + which) * workers + worker] = make_float2(m[t][e], l[t][e]);
+        } else {
           const int i = row / s.a.group, head = p.head * s.a.group + row % s.a.group;
           if (i < p.n) {
-            const float inv = top == -INFINITY ? 0.0f : 1.0f / den;
-            uint16_t* out = s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + head * s.a.o_stride_head + d;
-            uint2 u;
-            if (s.a.dtype == SPV_BF16) {
-              u.x = kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv);
-              u.y = kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv);
-            } else {
-              u.x = kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv);
-              u.y = kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv);
+            const float f = m[t][e] == -INFINITY ? 0.0f : vref / l[t][e];
+            uint16_t* out = s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + head * s.a.o_stride_head + r * kMine;
+#pragma unroll
+            for (int j = 0; j < kSteps; j += 4) {
+              uint32_t u[4];
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const float lo = o[j + x][t][e] * f, hi = o[j + x][t][e + 2] * f;
+                u[x] = s.a.dtype == SPV_BF16 ? kv_pack2<SPV_BF16>(lo, hi) : kv_pack2<SPV_FP16>(lo, hi);
+              }
+              *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(u[0], u[1], u[2], u[3]);
             }
-            *reinterpret_cast<uint2*>(out) = u;
-            if (d == 0) {
+            if (r == 0) {
               if (s.a.lse)
                 s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + head] =
-                    top == -INFINITY ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
-              s.pair_ml[(size_t)(p.b * c.kv_heads + p.head) * kRows + row] = make_float2(top, den);
+                    m[t][e] == -INFINITY ? -INFINITY : (m[t][e] + log2f(l[t][e])) * 0.6931471805599453f;
+              s.pair_ml[pair + row] = make_float2(m[t][e], l[t][e]);
             }
           }
-        } else {
-          *reinterpret_cast<float4*>(s.part_o + ((size_t)slot * kRows + row) * D + d) = sum;
-          if (d == 0) s.part_ml[(size_t)slot * kRows + row] = make_float2(top, den);
         }
       }
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(kWarps * 32) : "memory");     // sml is read no more
+  }
+  // nothing of this warp is in flight when it ends: a wait that gave up may leave copies behind
+  if (*abort_flag != 0u && lane == 0) {
+    for (int i = 0; i < L::kOwn; ++i)
+      for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(full + own + i, 0, 1000u) &&
+                          !mbar_try_wait_parked(full + own + i, 1, 1000u); ++tries) {
+      }
   }
 }
 
 // ---- pieces and weights --------------------------------------------------------------------------
 constexpr int kFinishThreads = 256;
-constexpr int kFinishKeys = 1024;
+__host__ __device__ constexpr int finish_workers(int row_slots) { return warps_of(row_slots) / 4; }   // of a block: four blocks an SM
 
-// grid (parts of the slots, key heads * batch); the first part also joins the pieces
+__device__ __forceinline__ const float2* part_ml(const StreamArgs& s, int workers, int row, int worker, int c0) {
+  return s.part_ml + (size_t)(2 * row + (worker == c0)) * workers + worker;
+}
+// Maximum and sum of a row over the pieces of a pair, those of workers c0 .. c1; a whole warp.
+__device__ __forceinline__ float2 joined(const StreamArgs& s, int workers, int c0, int c1, int row) {
+  const int lane = threadIdx.x & 31;
+  float top = -INFINITY, den = 0.0f;
+  for (int i = c0 + lane; i <= c1; i += 128) {
+    float2 ml[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) ml[x] = i + 32 * x <= c1 ? *part_ml(s, workers, row, i + 32 * x, c0) : make_float2(-INFINITY, 0.0f);
+    const float m = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    den *= exp2_fast(top - ref);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) den += ml[x].y * exp2_fast(ml[x].x - ref);
+    top = m;
+  }
+  float all = top;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+  den *= exp2_fast(top - (all == -INFINITY ? 0.0f : all));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+  return make_float2(all, den);
+}
+
+// A sequence without a tile: no keys (zeros) or no queries (the weights stay as they are).
 template <int D>
-__global__ void __launch_bounds__(kFinishThreads) kv_finish_kernel(const KvView c, const StreamArgs s, int ctas, int row_slots) {
+__device__ __forceinline__ void write_empty(const KvView& c, const KvAttnArgs& a, int b) {
+  const int n = seq_queries(a, b), len = seq_len(c, b);
+  for (int x = threadIdx.x; x < n * a.heads * (D / 8); x += blockDim.x) {
+    const int i = x / (a.heads * (D / 8)), h = x / (D / 8) % a.heads, d = x % (D / 8) * 8;
+    *reinterpret_cast<uint4*>(a.o + b * a.o_stride_b + i * a.o_stride_tok + h * a.o_stride_head + d) = make_uint4(0u, 0u, 0u, 0u);
+    if (a.lse && d == 0) a.lse[((size_t)b * a.tokens + i) * a.heads + h] = -INFINITY;
+  }
+  if (!a.w_out || n > 0) return;
+  for (int x = threadIdx.x; x < len; x += blockDim.x)
+    for (int h = 0; h < c.kv_heads; ++h) {
+      const int64_t at = b * a.w_stride_b + h * a.w_stride_head + x;
+      a.w_out[at] = a.w_in ? a.w_in[at] : 0.0f;
+    }
+}
+
+// A block takes the stretches of a few workers; half of its threads joins pieces while the other makes weights.
+template <int D>
+__global__ void __launch_bounds__(kFinishThreads, 4)
+    kv_finish_kernel(const KvView c, const StreamArgs s, int workers, int row_slots) {
   constexpr int kTile = tile_of(D);
-  __shared__ float2 stat[kKvStreamMaxRows];       // maximum, 1 / sum of a row
-  const int pair = blockIdx.y, b = pair / c.kv_heads, head = pair % c.kv_heads;
-  const int len = seq_len(c, b), n = seq_queries(s.a, b), rows = n * s.a.group;
-  const int key0 = blockIdx.x * kFinishKeys;
-  const bool weights = s.a.w_out != nullptr && key0 < len;
-  // tiles before this sequence: those of the sequences 0 .. b - 1
-  int64_t before = 0, all = 0;
-  for (int i = threadIdx.x; i < s.a.batch; i += kFinishThreads) {
-    const int64_t t = (int64_t)c.kv_heads * seq_key_tiles<kTile>(c, s.a, i);
-    all += t;
-    if (i < b) before += t;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-    all += __shfl_xor_sync(0xffffffffu, all, o);
-  }
-  __shared__ int64_t sums[kFinishThreads / 32][2];
-  if ((threadIdx.x & 31) == 0) { sums[threadIdx.x >> 5][0] = before; sums[threadIdx.x >> 5][1] = all; }
-  __syncthreads();
-  before = all = 0;
-#pragma unroll
-  for (int w = 0; w < kFinishThreads / 32; ++w) { before += sums[w][0]; all += sums[w][1]; }
-  const int tiles = seq_key_tiles<kTile>(c, s.a, b);
-  const int64_t line = before + (int64_t)head * tiles;
-  const int working = working_ctas(all, ctas);
-  const int c0 = tiles ? tile_owner(all, line, working) : 0, c1 = tiles ? tile_owner(all, line + tiles - 1, working) : 0;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  __shared__ float2 stat[kKvStreamMaxRows];     // maximum, 1 / sum of a row
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (weights || (blockIdx.x == 0 && c0 != c1)) {
+  for (int b = blockIdx.x; b < s.a.batch; b += gridDim.x)
+    if (seq_key_tiles<kTile>(c, s.a, b) == 0) write_empty<D>(c, s.a, b);
+  const int first = blockIdx.x * finish_workers(row_slots);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const Stretch at = s.stretch[first];
+  const Share share(at.total, workers);
+  if (first >= share.working) return;
+  Walk w;
+  w.pos = share.begin(first);
+  w.end = share.begin(min(first + finish_workers(row_slots), share.working));
+  w.before = at.before;
+  w.b = at.b;
+  Piece p{at.b, at.head, at.len, at.n, at.tiles, at.kt0, min(at.tiles, at.kt0 + w.end - w.pos), w.pos - at.kt0};
+  w.pos += p.kt1 - p.kt0;
+  const int joiners = s.a.w_out ? kFinishThreads / 2 : kFinishThreads;
+  bool more = true;
+  for (; more; more = next_piece<kTile>(c, s.a, w, p)) {
+    const int c0 = share.owner(p.line), c1 = share.owner(p.line + p.tiles - 1);
+    if (c0 == c1 && !s.a.w_out) continue;
+    const int rows = p.n * s.a.group;
+    const size_t pair = (size_t)(p.b * c.kv_heads + p.head) * row_slots;
+    __syncthreads();                            // stat of the piece before is read no more
     for (int row = warp; row < rows; row += kFinishThreads / 32) {
-      float top = -INFINITY, den = 0.0f;
-      if (c0 == c1) {
-        if (tiles) {
-          const float2 ml = s.pair_ml[(size_t)pair * row_slots + row];
-          top = ml.x;
-          den = ml.y;
-        }
-      } else {
-        for (int i = c0 + lane; i <= c1; i += 32) top = fmaxf(top, s.part_ml[(size_t)(2 * i + (i == c0)) * row_slots + row].x);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        for (int i = c0 + lane; i <= c1; i += 32) {
-          const float2 ml = s.part_ml[(size_t)(2 * i + (i == c0)) * row_slots + row];
-          den += ml.x == -INFINITY ? 0.0f : ml.y * exp2_fast(ml.x - top);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-      }
+      const float2 ml = c0 == c1 ? s.pair_ml[pair + row] : joined(s, workers, c0, c1, row);
       if (lane == 0) {
-        stat[row] = make_float2(top == -INFINITY ? 0.0f : top, top == -INFINITY ? 0.0f : 1.0f / den);
-        if (blockIdx.x == 0 && c0 != c1 && s.a.lse) {
-          const int i = row / s.a.group, h = head * s.a.group + row % s.a.group;
-          s.a.lse[((size_t)b * s.a.tokens + i) * s.a.heads + h] = top == -INFINITY ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+        stat[row] = make_float2(ml.x == -INFINITY ? 0.0f : ml.x, ml.x == -INFINITY ? 0.0f : 1.0f / ml.y);
+        if (c0 != c1 && p.kt0 == 0 && s.a.lse) {
+          const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
+          s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + h] =
+              ml.x == -INFINITY ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
         }
       }
     }
-  }
-  __syncthreads();
-  if (blockIdx.x == 0 && (c0 != c1 || tiles == 0)) {
-    for (int x = threadIdx.x; x < rows * (D / 4); x += kFinishThreads) {
-      const int row = x / (D / 4), d = x % (D / 4) * 4;
-      const int i = row / s.a.group, h = head * s.a.group + row % s.a.group;
+    __syncthreads();
+    if ((int)threadIdx.x < joiners) {
+      if (c0 == c1) continue;
+      // the blocks that meet the pair share its columns (four values of a row), and as many threads as there are share
+      // a column's pieces
+      const int f0 = c0 / finish_workers(row_slots), f1 = c1 / finish_workers(row_slots), mine = blockIdx.x - f0;
+      const int columns = rows * (D / 4);
+      const int x0 = columns * mine / (f1 - f0 + 1), x1 = columns * (mine + 1) / (f1 - f0 + 1);
+      const int lanes = x1 - x0 >= joiners ? 1 : min(32, 1 << (31 - __clz(joiners / max(1, x1 - x0))));
+      const int sub = threadIdx.x & (lanes - 1);
+      for (int xb = x0; xb < x1; xb += joiners / lanes) {
+        const int x = xb + (int)threadIdx.x / lanes;
+        const int row = x / (D / 4), d = x % (D / 4) * 4;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (x < x1) {
+          const float2 st = stat[row];
+#pragma unroll 4
+          for (int y = c0 + sub; y <= c1; y += lanes) {
+            const float m = part_ml(s, workers, row, y, c0)->x;
+            const float4 v = *reinterpret_cast<const float4*>(s.part_o + ((size_t)(2 * y + (y == c0)) * row_slots + row) * D + d);
+            const float f = exp2_fast(m - st.x) * st.y;
+            sum.x = fmaf(v.x, f, sum.x);
+            sum.y = fmaf(v.y, f, sum.y);
+            sum.z = fmaf(v.z, f, sum.z);
+            sum.w = fmaf(v.w, f, sum.w);
+          }
+        }
+        for (int o = lanes >> 1; o > 0; o >>= 1) {
+          sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
+          sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
+          sum.z += __shfl_xor_sync(0xffffffffu, sum.z, o);
+          sum.w += __shfl_xor_sync(0xffffffffu, sum.w, o);
+        }
+        if (x < x1 && sub == 0) {
+          const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
+          uint2 u;
+          if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x, sum.y), kv_pack2<SPV_BF16>(sum.z, sum.w));
+          else u = make_uint2(kv_pack2<SPV_FP16>(sum.x, sum.y), kv_pack2<SPV_FP16>(sum.z, sum.w));
+          *reinterpret_cast<uint2*>(s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + d) = u;
+        }
+      }
+      continue;
+    }
+    const int64_t wat = p.b * s.a.w_stride_b + p.head * s.a.w_stride_head;
+    const int key1 = min(p.len, p.kt1 * kTile);
+    const float* w_in = s.a.w_in ? s.a.w_in + wat : nullptr;
+    float* w_out = s.a.w_out + wat;
+    const bool wide = (((uintptr_t)w_out | (uintptr_t)w_in) & 15u) == 0;
+    // four keys a thread: the scores of a row are side by side
+    for (int key = p.kt0 * kTile + ((int)threadIdx.x - joiners) * 4; key < key1; key += joiners * 4) {
+      const float* zt = s.z + (size_t)(p.line + key / kTile) * s.rows * kTile + key % kTile;
+      const bool four = wide && key + 4 <= key1;
+      float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (w_in) {
+        if (four) {
+          w = *reinterpret_cast<const float4*>(w_in + key);
+        } else {
+          w.x = w_in[key];
+          if (key + 1 < key1) w.y = w_in[key + 1];
+          if (key + 2 < key1) w.z = w_in[key + 2];
+          if (key + 3 < key1) w.w = w_in[key + 3];
+        }
+      }
       float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (tiles) {
+#pragma unroll 4
+      for (int row = 0; row < rows; ++row) {
+        const float4 z = *reinterpret_cast<const float4*>(zt + row * kTile);
         const float2 st = stat[row];
-#pragma unroll 8
-        for (int y = c0; y <= c1; ++y) {
-          const size_t at = (size_t)(2 * y + (y == c0)) * row_slots + row;
-          const float m = s.part_ml[at].x;
-          const float f = m == -INFINITY ? 0.0f : exp2_fast(m - st.x) * st.y;
-          const float4 v = *reinterpret_cast<const float4*>(s.part_o + at * D + d);
-          sum.x = fmaf(v.x, f, sum.x);
-          sum.y = fmaf(v.y, f, sum.y);
-          sum.z = fmaf(v.z, f, sum.z);
-          sum.w = fmaf(v.w, f, sum.w);
-        }
-      } else if (d == 0 && s.a.lse) {
-        s.a.lse[((size_t)b * s.a.tokens + i) * s.a.heads + h] = -INFINITY;
+        sum.x = fmaf(exp2_fast(z.x - st.x), st.y, sum.x);
+        sum.y = fmaf(exp2_fast(z.y - st.x), st.y, sum.y);
+        sum.z = fmaf(exp2_fast(z.z - st.x), st.y, sum.z);
+        sum.w = fmaf(exp2_fast(z.w - st.x), st.y, sum.w);
       }
-      uint2 u;
-      if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x, sum.y), kv_pack2<SPV_BF16>(sum.z, sum.w));
-      else u = make_uint2(kv_pack2<SPV_FP16>(sum.x, sum.y), kv_pack2<SPV_FP16>(sum.z, sum.w));
-      *reinterpret_cast<uint2*>(s.a.o + b * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + d) = u;
-    }
-  }
-  if (!weights) return;
-  const int64_t wat = b * s.a.w_stride_b + head * s.a.w_stride_head;
-#pragma unroll
-  for (int x = 0; x < kFinishKeys / kFinishThreads; ++x) {
-    const int key = key0 + x * kFinishThreads + threadIdx.x;
-    if (key < len) {
-      const float* zt = s.z + (size_t)(line + key / kTile) * s.rows * kTile + key % kTile;
-      float w = 0.0f;
-      if (tiles) {
-#pragma unroll 8
-        for (int row = 0; row < rows; ++row) w += exp2_fast(zt[row * kTile] - stat[row].x) * stat[row].y;
+      w = make_float4(w.x + sum.x, w.y + sum.y, w.z + sum.z, w.w + sum.w);
+      if (four) {
+        *reinterpret_cast<float4*>(w_out + key) = w;
+      } else {
+        w_out[key] = w.x;
+        if (key + 1 < key1) w_out[key + 1] = w.y;
+        if (key + 2 < key1) w_out[key + 2] = w.z;
+        if (key + 3 < key1) w_out[key + 3] = w.w;
       }
-      s.a.w_out[wat + key] = (s.a.w_in ? s.a.w_in[wat + key] : 0.0f) + w;
     }
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// CTAs the plan is made for: the workspace is sized without a device, so by the largest GPU of this generation.
-constexpr int kMaxCtas = 160;
+// SMs the plan is made for: the workspace is sized without a device, so by the largest GPU of this generation.
+constexpr int kMaxSms = 160;
 
 int row_slots_of(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32); }
 
-struct Workspace { size_t part_o, part_ml, pair_ml, z, total; };
+struct Workspace { size_t part_o, part_ml, pair_ml, stretch, z, total; };
 Workspace plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d, bool weights) {
   const int rows = d->tokens * (d->heads / c->kv_heads), slots = row_slots_of(rows), tile = tile_of(c->head_dim);
   const size_t tiles = (size_t)q->batch * c->kv_heads * ((spv_kv_max_length(c, q) + tile - 1) / tile);
   Workspace w;
+  const size_t workers = (size_t)kMaxSms * warps_of(slots);
   w.part_o = 0;
-  w.part_ml = w.part_o + spv_align_up((size_t)kMaxCtas * kPartSlots * slots * c->head_dim * sizeof(float), 256);
-  w.pair_ml = w.part_ml + spv_align_up((size_t)kMaxCtas * kPartSlots * slots * sizeof(float2), 256);
-  w.z = w.pair_ml + spv_align_up((size_t)q->batch * c->kv_heads * slots * sizeof(float2), 256);
+  w.part_ml = w.part_o + spv_align_up(workers * kPartSlots * slots * c->head_dim * sizeof(float), 256);
+  w.pair_ml = w.part_ml + spv_align_up(workers * kPartSlots * slots * sizeof(float2), 256);
+  w.stretch = w.pair_ml + spv_align_up((size_t)q->batch * c->kv_heads * slots * sizeof(float2), 256);
+  w.z = w.stretch + spv_align_up(workers * sizeof(Stretch), 256);
   w.total = w.z + (weights ? spv_align_up(tiles * rows * tile * sizeof(float), 256) : 0);
   return w;
 }
@@ -866,6 +882,7 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   s.part_o = (float*)(base + w.part_o);
   s.part_ml = (float2*)(base + w.part_ml);
   s.pair_ml = (float2*)(base + w.pair_ml);
+  s.stretch = (Stretch*)(base + w.stretch);
   s.z = a.w_out ? (float*)(base + w.z) : nullptr;
   // a row of the map is 128 bytes: one slot of 128, or two of 64
   const uint64_t lines = (uint64_t)cache->pages * cache->kv_heads * cache->block * cache->head_dim / 128;
@@ -879,7 +896,7 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if (st != SPV_OK) return st;
   if ((st = spv_make_tmap_u8(ctx, &mv, cache->v, 2, dims, strides, box)) != SPV_OK) return st;
   const int64_t most = (int64_t)seqs->batch * cache->kv_heads * ((view.max_length + tile - 1) / tile);
-  int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+  int ctas = ctx->sm_count < kMaxSms ? ctx->sm_count : kMaxSms;
   if (most < ctas) ctas = (int)most;
   const int slots = row_slots_of(s.rows);
   auto go = [&](auto fmt, auto dim) -> int32_t {
@@ -897,7 +914,9 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if (st != SPV_OK) return st;
   // the second kernel's launch overlaps the first; it waits on the device for the first to end
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.w_out ? (view.max_length + kFinishKeys - 1) / kFinishKeys : 1, cache->kv_heads * seqs->batch);
+  const int workers = ctas * warps_of(slots);
+  const int64_t used = most < workers ? most : workers;
+  cfg.gridDim = dim3((unsigned)((used + finish_workers(slots) - 1) / finish_workers(slots)));
   cfg.blockDim = dim3(kFinishThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -905,7 +924,7 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  SPV_CUDA_OK(cache->head_dim == 64 ? cudaLaunchKernelEx(&cfg, kv_finish_kernel<64>, view, s, ctas, slots)
-                                    : cudaLaunchKernelEx(&cfg, kv_finish_kernel<128>, view, s, ctas, slots));
+  SPV_CUDA_OK(cache->head_dim == 64 ? cudaLaunchKernelEx(&cfg, kv_finish_kernel<64>, view, s, workers, slots)
+                                    : cudaLaunchKernelEx(&cfg, kv_finish_kernel<128>, view, s, workers, slots));
   return spv_launch_ok(ctx, 2);
 }
