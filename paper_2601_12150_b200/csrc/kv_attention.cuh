@@ -22,6 +22,11 @@ size_t spv_kv_stream_workspace(const spv_kv_cache* cache, const spv_kv_seqs* seq
 int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs, const KvAttnArgs& a,
                           void* workspace, cudaStream_t stream);
 
+// ---- the tiled form (many query rows per key head), kv_attention_prompt.cu ----
+size_t spv_kv_prompt_workspace(const spv_kv_cache* cache, const spv_kv_seqs* seqs, const spv_kv_attn_desc* d);
+int32_t spv_kv_prompt_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs, const spv_kv_attn_desc* d,
+                          const KvAttnArgs& a, void* workspace, cudaStream_t stream);
+
 #ifdef __CUDACC__
 namespace spv {
 

@@ -1,0 +1,920 @@
+// Attention of many query rows over the 8-bit cache: prompts.
+//
+// Bound by the tensor cores and the exponentials: 4 * head_dim operations and one exponential a (row, key), and for the
+// weights 2 * head_dim and one exponential more (a row's weights are known only after its last key).
+//
+//   kv_prompt_prepare    the sequences' codes as dense fp16, keys and values scaled by one power of two of their sequence
+//                        and head, queries by one of their row: exact but for what lies 2^-24 below.  Every key tile is
+//                        read by rows / 256 CTAs; converting it in each of them would cost more than half of the issue
+//                        slots that the softmax needs (1.4 instructions a code against 5 a score).
+//   kv_prompt_attend     one CTA per SM.  Units of 256 query rows x 128 keys form a line, and every CTA takes an equal
+//                        stretch of it.  Two row blocks of 128 take turns: while the eight warps of softmax work on one
+//                        block's scores (TMEM, a thread per row), the tensor cores do the other's S = Q K^T and
+//                        O += P V (P stays in TMEM, over its S).
+//   kv_prompt_join       units that were cut between CTAs.
+//   kv_prompt_weigh      weights: S^T = K Q^T by tiles of 128 keys, so that a key's scores are a thread's own and its
+//                        sum over the rows needs no other thread; 2^(z - lse) with the rows' lse from before.
+#include <type_traits>
+
+#include "kv_attention.cuh"
+
+namespace {
+
+using namespace spv;
+
+constexpr int kRowsUnit = 256;             // two blocks of 128
+constexpr int kKeys = 128;
+constexpr int kMaxSms = 160;
+constexpr float kFloor = -1.0e30f;         // running maximum before the first key
+
+struct Desc {                              // last unit of a CTA's stretch
+  int total, b, head, unit, line, tiles, rows, n;
+};
+
+struct PromptArgs {
+  KvAttnArgs a;
+  int32_t b0, nb;                          // sequences of this round: b0 .. b0 + nb - 1
+  int32_t rows_pad, keys_pad;              // per (sequence, key head) in the dense copies
+  uint16_t* q16;                           // [nb * kv_heads][rows_pad][D]
+  uint16_t* k16;                           // [nb * kv_heads][keys_pad][D]
+  uint16_t* v16;
+  float* q_factor;                         // [nb * kv_heads][rows_pad]: softmax scale, log2 e and the row's power of two
+  float2* refs;                            // [nb * kv_heads]: units of the keys and of the values
+  float2* row_stat;                        // [nb * kv_heads][rows_pad]: score factor, -lse (log2 domain)
+  float* part_o;                           // [CTA][2][256][D]
+  float2* part_ml;                         // [CTA][2][256]
+  Desc* desc;                              // [CTA]
+};
+
+__device__ __forceinline__ int seq_len(const KvView& c, int b) { return spv_kv_clamp(__ldg(c.lengths + b), c.max_length); }
+__device__ __forceinline__ int seq_queries(const KvAttnArgs& a, int b) {
+  return a.counts ? spv_kv_clamp(__ldg(a.counts + b), a.tokens) : a.tokens;
+}
+__device__ __forceinline__ int padded_keys(int len) { return max(kKeys, (len + kKeys - 1) / kKeys * kKeys); }
+
+// ---- dense copies --------------------------------------------------------------------------------
+constexpr int kPrepThreads = 256;
+constexpr int kPrepRows = 64;
+
+__device__ __forceinline__ float block_max(float x, float* tmp) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPrepThreads / 32; ++i) x = fmaxf(x, tmp[i]);
+  return x;
+}
+
+// grid (key chunks + query chunks of 64, key heads, sequences)
+template <int FMT, int D>
+__global__ void __launch_bounds__(kPrepThreads) kv_prompt_prepare(const KvView c, const PromptArgs s, int key_chunks) {
+  const int head = blockIdx.y, bl = blockIdx.z, b = s.b0 + bl;
+  const size_t pair = (size_t)bl * c.kv_heads + head;
+  const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
+  const int n = s.a.counts ? kv_clamped(__ldg(s.a.counts + b), s.a.tokens, c.status) : s.a.tokens;
+  if (n == 0) return;
+  if ((int)blockIdx.x < key_chunks) {
+    __shared__ float tmp[2][kPrepThreads / 32];
+    const int base = blockIdx.x * kPrepRows;
+    if (base >= padded_keys(len)) return;
+    const int32_t* row = c.table + b * c.table_stride;
+    float ks = 0.0f, vs = 0.0f;
+    for (int col = threadIdx.x; col * s.a.block < len; col += kPrepThreads) {
+      const int page = kv_page(row, col, c.pages, c.status);
+      if (page >= 0) {
+        ks = fmaxf(ks, __ldg(c.k_scale + (size_t)page * c.kv_heads + head));
+        vs = fmaxf(vs, __ldg(c.v_scale + (size_t)page * c.kv_heads + head));
+      }
+    }
+    ks = block_max(ks, tmp[0]);
+    vs = block_max(vs, tmp[1]);
+    // the largest code of the largest block comes to just below 2^16: 24 and more powers of two are left below it
+    constexpr float kTop = FMT == SPV_KV_INT8 ? 256.0f : 128.0f;
+    const float k_unit = ks > 0.0f ? ks / kTop : 1.0f, v_unit = vs > 0.0f ? vs / kTop : 1.0f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) s.refs[pair] = make_float2(k_unit, v_unit);
+    constexpr int kVecRow = D / 16, kMine = kPrepRows * kVecRow / kPrepThreads;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int v = threadIdx.x + i * kPrepThreads, slot = base + v / kVecRow, col = v % kVecRow * 16;
+      uint4 x[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+      float f[2] = {0.0f, 0.0f};
+      const int page = slot < len ? __ldg(row + slot / s.a.block) : -1;
+      if (spv_kv_valid_page(page, c.pages)) {
+        const size_t ph = (size_t)page * c.kv_heads + head;
+        const size_t at = (size_t)spv_kv_row(page, c.kv_heads, head, s.a.block, slot) * D + col;
+        x[0] = __ldcs(reinterpret_cast<const uint4*>(c.k + at));
+        x[1] = __ldcs(reinterpret_cast<const uint4*>(c.v + at));
+        f[0] = __ldg(c.k_scale + ph) / k_unit;
+        f[1] = __ldg(c.v_scale + ph) / v_unit;
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint32_t w[4] = {x[m].x, x[m].y, x[m].z, x[m].w};
+        uint32_t u[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float y[4];
+          kv_decode4<FMT>(w[j], y);
+          u[2 * j] = kv_pack2<SPV_FP16>(y[0] * f[m], y[1] * f[m]);
+          u[2 * j + 1] = kv_pack2<SPV_FP16>(y[2] * f[m], y[3] * f[m]);
+        }
+        uint4* dst = reinterpret_cast<uint4*>((m ? s.v16 : s.k16) + (pair * s.keys_pad + slot) * D + col);
+        dst[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        dst[1] = make_uint4(u[4], u[5], u[6], u[7]);
+      }
+    }
+    return;
+  }
+  // queries: a warp per row
+  const int rows = n * s.a.group, row_end = (rows + kRowsUnit - 1) / kRowsUnit * kRowsUnit;
+  const int row0 = ((int)blockIdx.x - key_chunks) * kPrepRows;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int kPer = D / 32;
+  for (int row = row0 + warp; row < min(row0 + kPrepRows, row_end); row += kPrepThreads / 32) {
+    uint32_t w[kPer / 2];
+#pragma unroll
+    for (int e = 0; e < kPer / 2; ++e) w[e] = 0u;
+    if (row < rows) {
+      const int i = row / s.a.group, h = head * s.a.group + row % s.a.group;
+      const uint16_t* src = s.a.q + b * s.a.q_stride_b + i * s.a.q_stride_tok + h * s.a.q_stride_head + lane * kPer;
+#pragma unroll
+      for (int e = 0; e < kPer / 2; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
+    }
+    float x[kPer];
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < kPer / 2; ++e) {
+      const float2 f = s.a.dtype == SPV_BF16 ? kv_unpack2<SPV_BF16>(w[e]) : kv_unpack2<SPV_FP16>(w[e]);
+      x[2 * e] = f.x;
+      x[2 * e + 1] = f.y;
+      big = max(big, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
+    }
+    big = __reduce_max_sync(0xffffffffu, big);
+    const int ex = max((int)(big >> 23) - 127, -100);
+    const float up = kv_pow2(14 - ex);
+    uint32_t* dst = reinterpret_cast<uint32_t*>(s.q16 + (pair * s.rows_pad + row) * D + lane * kPer);
+#pragma unroll
+    for (int e = 0; e < kPer / 2; ++e) dst[e] = kv_pack2<SPV_FP16>(x[2 * e] * up, x[2 * e + 1] * up);
+    if (lane == 0) s.q_factor[pair * s.rows_pad + row] = s.a.scale * 1.4426950408889634f * kv_pow2(ex - 14);
+  }
+}
+
+// ---- the line of units -----------------------------------------------------------------------------
+// Key tiles of the unit whose rows are [unit * 256, ...): up to the last key that its last row sees, one at least.
+__device__ __forceinline__ int block_tiles(int len, int n, int group, int causal, int row0, int row1) {
+  const int rows = n * group;
+  if (row0 >= rows) return 0;
+  const int end = spv_kv_query_end(len, n, (min(row1, rows) - 1) / group, causal);
+  return max(1, (end + kKeys - 1) / kKeys);
+}
+__device__ __forceinline__ int unit_tiles(int len, int n, int group, int causal, int unit) {
+  return block_tiles(len, n, group, causal, unit * kRowsUnit, (unit + 1) * kRowsUnit);
+}
+__device__ __forceinline__ int seq_tiles(int len, int n, int group, int causal) {   // of one key head
+  const int units = (n * group + kRowsUnit - 1) / kRowsUnit;
+  if (!causal) return units * unit_tiles(len, n, group, 0, 0);
+  int sum = 0;
+  for (int u = 0; u < units; ++u) sum += unit_tiles(len, n, group, 1, u);
+  return sum;
+}
+
+struct Share {
+  int working, per, more;
+  __device__ __forceinline__ Share(int total, int workers) {
+    working = min(total, workers);
+    per = working ? total / working : 0;
+    more = working ? total % working : 0;
+  }
+  __device__ __forceinline__ int begin(int worker) const { return worker * per + min(worker, more); }
+  __device__ __forceinline__ int owner(int t) const {
+    const int wide = more * (per + 1);
+    return t < wide ? t / (per + 1) : more + (t - wide) / per;
+  }
+};
+
+struct Piece {
+  int b, head, unit, len, n;               // b within the round
+  int line, tiles, kt0, kt1;               // of the unit
+};
+struct Walk {
+  int pos, end, before, b;                 // before: tiles in front of sequence b
+  int head, unit, at;                      // unit that begins at `at` (-1: not yet looked up)
+};
+__device__ __forceinline__ bool next_piece(const KvView& c, const PromptArgs& s, Walk& w, Piece& p) {
+  if (w.pos >= w.end) return false;
+  for (;;) {
+    const int len = seq_len(c, s.b0 + w.b), n = seq_queries(s.a, s.b0 + w.b);
+    const int units = (n * s.a.group + kRowsUnit - 1) / kRowsUnit;
+    if (w.at < 0) {
+      const int per_head = n ? seq_tiles(len, n, s.a.group, s.a.causal) : 0;
+      if (w.pos >= w.before + c.kv_heads * per_head) {
+        w.before += c.kv_heads * per_head;
+        if (++w.b >= s.nb) return false;
+        continue;
+      }
+      w.head = (w.pos - w.before) / per_head;
+      w.unit = 0;
+      w.at = w.before + w.head * per_head;
+    }
+    while (w.unit < units) {
+      const int t = unit_tiles(len, n, s.a.group, s.a.causal, w.unit);
+      if (w.pos < w.at + t) {
+        p.b = w.b;
+        p.head = w.head;
+        p.unit = w.unit;
+        p.len = len;
+        p.n = n;
+        p.line = w.at;
+        p.tiles = t;
+        p.kt0 = w.pos - w.at;
+        p.kt1 = min(t, p.kt0 + w.end - w.pos);
+        w.pos += p.kt1 - p.kt0;
+        if (p.kt1 == t) {
+          w.at += t;
+          if (++w.unit == units) {
+            w.unit = 0;
+            if (++w.head == c.kv_heads) {
+              w.before = w.at;
+              ++w.b;
+              w.at = -1;
+              if (w.b >= s.nb) w.b = s.nb - 1, w.end = w.pos;
+            }
+          }
+        }
+        return true;
+      }
+      w.at += t;
+      ++w.unit;
+    }
+    return false;                            // not reached: every place of the line is in a unit
+  }
+}
+
+__host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
+  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// As smem_desc_sw128, for an MN-major operand of several 64-wide parts `part` bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_parts(uint32_t saddr, uint32_t part) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(part >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
+constexpr int kAttendThreads = 384;        // two warpgroups of softmax; producer, two issuers of products
+template <int D>
+struct AttendSmem {
+  static constexpr int kTile = 128 * D * 2;          // 128 rows of fp16: D / 64 parts of 128-byte rows
+  static constexpr int kStages = D == 128 ? 2 : 4;
+  static constexpr int oQ = 0;
+  static constexpr int oK = 2 * kTile;
+  static constexpr int oV = oK + kStages * kTile;
+  static constexpr int oBars = oV + kStages * kTile;
+  static constexpr int kTotal = oBars + 1024;
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* m, uint64_t* bar, int row) {
+#pragma unroll
+  for (int x = 0; x < D / 64; ++x) tma_load_2d(dst + x * 128 * 128, m, bar, x * 64, row);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kAttendThreads, 1)
+    kv_prompt_attend(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ CUtensorMap map_v, const KvView c, const PromptArgs s) {
+  using L = AttendSmem<D>;
+  constexpr int ST = L::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::oBars);
+  uint64_t* q_full = bars;                 // one for both blocks
+  uint64_t* q_empty = bars + 1;            // both issuers are through with Q
+  uint64_t* k_full = bars + 2;
+  uint64_t* k_empty = k_full + ST;
+  uint64_t* v_full = k_empty + ST;
+  uint64_t* v_empty = v_full + ST;
+  uint64_t* s_full = v_empty + ST;         // [2]
+  uint64_t* p_full = s_full + 2;           // [2]
+  uint64_t* o_full = p_full + 2;           // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  int* s_total = reinterpret_cast<int*>(tmem_slot + 2);
+  int* s_before = s_total + 1;
+  int* s_b = s_total + 2;
+  int* warp_sum = s_total + 4;             // [12]
+  uint32_t* status = c.status - 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 2);
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(k_full + i, 1);
+      mbar_init(k_empty + i, 2);
+      mbar_init(v_full + i, 1);
+      mbar_init(v_empty + i, 2);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 128);
+      mbar_init(o_full + i, 1);
+    }
+    *abort_flag = 0u;
+    mbar_fence_init();
+  }
+  if (warp == 8) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  // tiles of the sequences of this round, and where this CTA's stretch begins
+  {
+    const int per = (s.nb + kAttendThreads - 1) / kAttendThreads;
+    const int b0 = threadIdx.x * per, b1 = min(s.nb, b0 + per);
+    auto tiles = [&](int b) {
+      const int n = seq_queries(s.a, s.b0 + b);
+      return n ? c.kv_heads * seq_tiles(seq_len(c, s.b0 + b), n, s.a.group, s.a.causal) : 0;
+    };
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) sum += tiles(b);
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    int base = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kAttendThreads / 32; ++w) {
+      if (w < warp) base += warp_sum[w];
+      total += warp_sum[w];
+    }
+    const Share share(total, gridDim.x);
+    const int target = (int)blockIdx.x < share.working ? share.begin(blockIdx.x) : total;
+    int at = base + inc - sum;
+    if (target >= at && target < at + sum) {
+      int b = b0;
+      for (;; ++b) {
+        const int t = tiles(b);
+        if (target < at + t || b + 1 >= b1) break;
+        at += t;
+      }
+      *s_b = b;
+      *s_before = at;
+    }
+    if (threadIdx.x == 0) *s_total = total;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Share share(*s_total, gridDim.x);
+  Walk walk;
+  walk.pos = walk.end = 0;
+  if ((int)blockIdx.x < share.working) {
+    walk.pos = share.begin(blockIdx.x);
+    walk.end = share.begin(blockIdx.x + 1);
+    walk.before = *s_before;
+    walk.b = *s_b;
+    walk.at = -1;
+  }
+  Piece p;
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == 8) {
+      // ---- producer
+      if (lane == 0) {
+        tma_prefetch_desc(&map_q);
+        tma_prefetch_desc(&map_k);
+        tma_prefetch_desc(&map_v);
+        uint32_t kv = 0, pieces = 0;
+        while (next_piece(c, s, walk, p)) {
+          const int pair = p.b * c.kv_heads + p.head;
+          if (pieces) mbar_wait(q_empty, (pieces - 1) & 1, abort_flag, status, 0x4C00u);
+          mbar_expect_tx(q_full, 2 * L::kTile);
+          load_tile<D>(smem + L::oQ, &map_q, q_full, pair * s.rows_pad + p.unit * kRowsUnit);
+          load_tile<D>(smem + L::oQ + L::kTile, &map_q, q_full, pair * s.rows_pad + p.unit * kRowsUnit + 128);
+          ++pieces;
+          for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
+            const uint32_t st = kv % ST, ph = ((kv / ST) & 1) ^ 1;
+            const int row = pair * s.keys_pad + kt * kKeys;
+            mbar_wait(k_empty + st, ph, abort_flag, status, 0x4C01u);
+            mbar_expect_tx(k_full + st, L::kTile);
+            load_tile<D>(smem + L::oK + st * L::kTile, &map_k, k_full + st, row);
+            mbar_wait(v_empty + st, ph, abort_flag, status, 0x4C02u);
+            mbar_expect_tx(v_full + st, L::kTile);
+            load_tile<D>(smem + L::oV + st * L::kTile, &map_v, v_full + st, row);
+          }
+        }
+        // a wait that gave up may leave copies behind: they end before the CTA does
+        if (*abort_flag != 0u) {
+          for (int i = 0; i < 2 * ST; ++i) {
+            uint64_t* bar = i < ST ? k_full + i : v_full + i - ST;
+            for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(bar, 0, 1000u) && !mbar_try_wait_parked(bar, 1, 1000u); ++tries) {
+            }
+          }
+        }
+      }
+    } else if (warp < 11) {
+      // ---- products of one row block
+      if (lane == 0) {
+        const int x = warp - 9;
+        constexpr uint32_t idesc_s = idesc_f16(128, kKeys, false), idesc_o = idesc_f16(128, D, true);
+        const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * 128;
+        uint32_t kv = 0, pieces = 0, mine = 0;
+        while (next_piece(c, s, walk, p)) {
+          const int row0 = p.unit * kRowsUnit + x * 128;
+          const int tiles = block_tiles(p.len, p.n, s.a.group, s.a.causal, row0, row0 + 128);
+          mbar_wait(q_full, pieces & 1, abort_flag, status, 0x4C03u);
+          ++pieces;
+          const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + x * L::kTile));
+          for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
+            const uint32_t st = kv % ST, ph = (kv / ST) & 1;
+            if (kt >= tiles) {               // this block sees none of the tile
+              mbar_wait(k_full + st, ph, abort_flag, status, 0x4C04u);
+              mbar_arrive(k_empty + st);
+              mbar_wait(v_full + st, ph, abort_flag, status, 0x4C05u);
+              mbar_arrive(v_empty + st);
+              continue;
+            }
+            mbar_wait(k_full + st, ph, abort_flag, status, 0x4C06u);
+            tc_fence_after();
+            const uint64_t dk = smem_desc_sw128(smem_u32(smem + L::oK + st * L::kTile));
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);      // parts of 64 are 16 KB apart
+              mma_ss(t_s, dq + off, dk + off, idesc_s, kk != 0);
+            }
+            tc_commit(s_full + x);
+            tc_commit(k_empty + st);
+            mbar_wait(v_full + st, ph, abort_flag, status, 0x4C07u);
+            mbar_wait(p_full + x, mine & 1, abort_flag, status, 0x4C08u);
+            tc_fence_after();
+            const uint64_t dv = smem_desc_parts(smem_u32(smem + L::oV + st * L::kTile), 128 * 128);
+#pragma unroll
+            for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(t_o, t_s + kk * 8, dv + (uint64_t)(kk * 128), idesc_o, (kt > p.kt0) | (kk != 0));
+            tc_commit(v_empty + st);
+            ++mine;
+          }
+          if (min(tiles, p.kt1) > p.kt0) tc_commit(o_full + x);
+          tc_commit(q_empty);
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ---- softmax: a thread per row
+    const int x = warp >> 2, row_in = (warp & 3) * 32 + lane;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + x * 128 + lane_off, t_o = tmem + 256 + x * 128 + lane_off;
+    uint32_t mine = 0, outs = 0;
+    while (next_piece(c, s, walk, p)) {
+      const int pair = p.b * c.kv_heads + p.head;
+      const int block0 = p.unit * kRowsUnit + x * 128, row = block0 + row_in, rows = p.n * s.a.group;
+      const int tiles = min(p.kt1, block_tiles(p.len, p.n, s.a.group, s.a.causal, block0, block0 + 128));
+      const bool real = row < rows;
+      const float2 ref = s.refs[pair];
+      const float f = real ? s.q_factor[(size_t)pair * s.rows_pad + row] * ref.x : 0.0f;
+      const int end = real ? spv_kv_query_end(p.len, p.n, row / s.a.group, s.a.causal) : p.len;
+      float m = kFloor, l = 0.0f;
+      for (int kt = p.kt0; kt < tiles; ++kt, ++mine) {
+        mbar_wait(s_full + x, mine & 1, abort_flag, status, 0x4C09u);
+        __syncwarp();
+        tc_fence_after();
+        uint32_t z[kKeys];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32 * i, z + 32 * i);
+        tc_wait_ld();
+        const int see = end - kt * kKeys;
+        if (see < kKeys) {
+#pragma unroll
+          for (int i = 0; i < kKeys; ++i)
+            if (i >= see) z[i] = 0xff800000u;
+        }
+        float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kKeys; i += 8) {
+          t0 = max3(t0, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
+          t1 = max3(t1, __uint_as_float(z[i + 2]), __uint_as_float(z[i + 3]));
+          t2 = max3(t2, __uint_as_float(z[i + 4]), __uint_as_float(z[i + 5]));
+          t3 = max3(t3, __uint_as_float(z[i + 6]), __uint_as_float(z[i + 7]));
+        }
+        // the maximum is renewed only where it would grow by more than 2^8; every product before this S has completed,
+        // so the results may be rescaled at once
+        const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f;
+        const bool need = top > m + 8.0f;
+        const float m_new = need ? top : m;
+        const float alpha = need ? exp2_fast(m - m_new) : 1.0f;
+        if (__any_sync(0xffffffffu, need && l > 0.0f)) {
+#pragma unroll
+          for (int i = 0; i < D / 16; ++i) {
+            uint32_t o[16];
+            tmem_ld16(t_o + 16 * i, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st16(t_o + 16 * i, o);
+          }
+        }
+        m = m_new;
+        float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
+        const float2 f2 = make_float2(f, f), nm = make_float2(-m, -m);
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) {
+            const uint32_t* y = z + 32 * h + i;
+            const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), f2, nm);
+            const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), f2, nm);
+            const float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y));
+            const float2 p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
+            sum0 = __fadd2_rn(sum0, p0);
+            sum1 = __fadd2_rn(sum1, p1);
+            pk[i / 2] = kv_pack2<SPV_FP16>(p0.x, p0.y);
+            pk[i / 2 + 1] = kv_pack2<SPV_FP16>(p1.x, p1.y);
+          }
+          tmem_st16(t_s + 16 * h, pk);
+        }
+        l = l * alpha + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
+        tc_wait_st();
+        tc_fence_before();
+        mbar_arrive(p_full + x);
+      }
+      // ---- results of the piece
+      const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
+      const size_t slot = ((size_t)(2 * blockIdx.x + (p.kt0 > 0 ? 0 : 1)) * kRowsUnit) + x * 128 + row_in;
+      const bool any = tiles > p.kt0;        // uniform: the block saw a tile of the piece
+      if (any) {
+        mbar_wait(o_full + x, outs & 1, abort_flag, status, 0x4C0Au);
+        ++outs;
+        tc_fence_after();
+      }
+      const float inv = l > 0.0f ? ref.y / l : 0.0f;
+      const int i_q = row / s.a.group, h_q = p.head * s.a.group + row % s.a.group;
+      uint16_t* out = s.a.o + (s.b0 + p.b) * s.a.o_stride_b + i_q * s.a.o_stride_tok + h_q * s.a.o_stride_head;
+      if (any) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          uint32_t o[16];
+          __syncwarp();
+          tmem_ld16(t_o + 16 * i, o);
+          tc_wait_ld();
+          if (!whole) {
+            float4* at = reinterpret_cast<float4*>(s.part_o + slot * D + 16 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              at[e] = make_float4(__uint_as_float(o[4 * e]), __uint_as_float(o[4 * e + 1]), __uint_as_float(o[4 * e + 2]),
+                                  __uint_as_float(o[4 * e + 3]));
+          } else if (real) {
+            uint32_t u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float lo = l > 0.0f ? __uint_as_float(o[2 * e]) * inv : 0.0f;
+              const float hi = l > 0.0f ? __uint_as_float(o[2 * e + 1]) * inv : 0.0f;
+              u[e] = s.a.dtype == SPV_BF16 ? kv_pack2<SPV_BF16>(lo, hi) : kv_pack2<SPV_FP16>(lo, hi);
+            }
+            reinterpret_cast<uint4*>(out + 16 * i)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+            reinterpret_cast<uint4*>(out + 16 * i)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+          }
+        }
+      }
+      if (!whole) {
+        s.part_ml[slot] = make_float2(l > 0.0f ? m : -INFINITY, l);
+      } else {
+        const float lse = l > 0.0f ? m + log2f(l) : -INFINITY;
+        if (real && s.a.lse) s.a.lse[((size_t)(s.b0 + p.b) * s.a.tokens + i_q) * s.a.heads + h_q] = lse * 0.6931471805599453f;
+        s.row_stat[(size_t)pair * s.rows_pad + row] = real && l > 0.0f ? make_float2(f, -lse) : make_float2(0.0f, -INFINITY);
+      }
+    }
+    if (threadIdx.x == 0) {
+      Desc d = {*s_total, 0, 0, 0, 0, 0, 0, 0};
+      if ((int)blockIdx.x < share.working) d = Desc{*s_total, p.b, p.head, p.unit, p.line, p.tiles, p.n * s.a.group, p.n};
+      s.desc[blockIdx.x] = d;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_dealloc(tmem, 512);
+}
+
+// ---- units that were cut: grid (CTA, 16 rows) ---------------------------------------------------------
+template <int D>
+__global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const PromptArgs s, int ctas) {
+  const Desc d = s.desc[blockIdx.x];
+  const Share share(d.total, ctas);
+  if ((int)blockIdx.x >= share.working) return;
+  const int c0 = share.owner(d.line), c1 = share.owner(d.line + d.tiles - 1);
+  if (c0 != (int)blockIdx.x || c0 == c1) return;
+  const int pair = d.b * c.kv_heads + d.head;
+  const float2 ref = s.refs[pair];
+  constexpr int kLanes = D / 4;
+  for (int r = threadIdx.x / kLanes; r < 16; r += 256 / kLanes) {
+    const int in = blockIdx.y * 16 + r, row = d.unit * kRowsUnit + in, col = threadIdx.x % kLanes * 4;
+    float top = -INFINITY;
+    for (int i = c0; i <= c1; ++i) top = fmaxf(top, s.part_ml[(size_t)(2 * i + (i == c0)) * kRowsUnit + in].x);
+    float den = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int i = c0; i <= c1; ++i) {
+      const size_t slot = (size_t)(2 * i + (i == c0)) * kRowsUnit + in;
+      const float2 ml = s.part_ml[slot];
+      if (ml.y > 0.0f || ml.y != ml.y) {                   // without a key nothing was written
+        const float f = exp2_fast(ml.x - (top == -INFINITY ? 0.0f : top));
+        const float4 v = *reinterpret_cast<const float4*>(s.part_o + slot * D + col);
+        den = fmaf(ml.y, f, den);
+        sum.x = fmaf(v.x, f, sum.x);
+        sum.y = fmaf(v.y, f, sum.y);
+        sum.z = fmaf(v.z, f, sum.z);
+        sum.w = fmaf(v.w, f, sum.w);
+      }
+    }
+    const bool some = den > 0.0f || den != den;
+    const bool real = row < d.rows;
+    if (real) {
+      const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
+      const float inv = some ? ref.y / den : 0.0f;
+      uint2 u;
+      if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv));
+      else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv));
+      *reinterpret_cast<uint2*>(s.a.o + (s.b0 + d.b) * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + col) = u;
+      if (col == 0 && s.a.lse)
+        s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    }
+    if (col == 0) {
+      const size_t at = (size_t)pair * s.rows_pad + row;
+      s.row_stat[at] = real && some ? make_float2(s.q_factor[at] * ref.x, -(top + log2f(den))) : make_float2(0.0f, -INFINITY);
+    }
+  }
+}
+
+// ---- weights: grid (key tiles, key heads, sequences), two CTAs an SM ------------------------------------
+constexpr int kWeighThreads = 192;         // four warps of sums (a thread per key), producer, issuer
+template <int D>
+struct WeighSmem {
+  static constexpr int kTile = 128 * D * 2;
+  static constexpr int kStages = 2;
+  static constexpr int oQ = kTile;
+  static constexpr int oStat = oQ + kStages * kTile;       // row_stat of the tile, by pairs of rows: f, f', -lse, -lse'
+  static constexpr int oBars = oStat + kStages * 128 * 8;
+  static constexpr int kTotal = oBars + 256;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kWeighThreads, 2)
+    kv_prompt_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const KvView c,
+                    const PromptArgs s) {
+  using L = WeighSmem<D>;
+  constexpr int ST = L::kStages;
+  const int head = blockIdx.y, b = s.b0 + blockIdx.z, key0 = blockIdx.x * kKeys;
+  const int pair = blockIdx.z * c.kv_heads + head;
+  const int len = seq_len(c, b), n = seq_queries(s.a, b), rows = n * s.a.group;
+  if (key0 >= len) return;
+  // rows that see a key: those from (key - (len - n)) * group on, where the mask is causal
+  auto first_row = [&](int key) { return s.a.causal ? (int)max((int64_t)0, ((int64_t)key - len + n) * s.a.group) : 0; };
+  const int t0 = min(first_row(key0), rows) / 128, t1 = (rows + 127) / 128;
+  const int key = key0 + threadIdx.x;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::oBars);
+  uint64_t* k_full = bars;
+  uint64_t* q_full = bars + 1;             // [ST] tile and row_stat
+  uint64_t* q_empty = q_full + ST;         // [ST] product done and row_stat read
+  uint64_t* s_full = q_empty + ST;         // [2]
+  uint64_t* s_empty = s_full + 2;          // [2]
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_empty + 2);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* status = c.status - 1;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(k_full, 1);
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(q_full + i, 2);
+      mbar_init(q_empty + i, 1 + 128);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + i, 1);
+      mbar_init(s_empty + i, 128);
+    }
+    *abort_flag = 0u;
+    mbar_fence_init();
+  }
+  if (warp == 5) {
+    tmem_alloc(tmem_slot, 256);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  if (warp == 4) {
+    if (lane == 0 && t0 < t1) {
+      mbar_expect_tx(k_full, L::kTile);
+      load_tile<D>(smem, &map_k, k_full, pair * s.keys_pad + key0);
+    }
+    for (int t = t0; t < t1; ++t) {
+      const uint32_t j = t - t0, st = j % ST;
+      mbar_wait(q_empty + st, ((j / ST) & 1) ^ 1, abort_flag, status, 0x4D00u);
+      if (lane == 0) {
+        mbar_expect_tx(q_full + st, L::kTile);
+        load_tile<D>(smem + L::oQ + st * L::kTile, &map_q, q_full + st, pair * s.rows_pad + t * 128);
+      }
+      float4* stat = reinterpret_cast<float4*>(smem + L::oStat + st * 1024);
+      const float4* src = reinterpret_cast<const float4*>(s.row_stat + (size_t)pair * s.rows_pad + t * 128);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float4 v = src[lane + 32 * i];
+        stat[lane + 32 * i] = make_float4(v.x, v.z, v.y, v.w);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_full + st);
+      __syncwarp();
+    }
+  } else if (warp == 5) {
+    if (lane == 0 && t0 < t1) {
+      constexpr uint32_t idesc = idesc_f16(128, 128, false);
+      const uint64_t dk = smem_desc_sw128(smem_u32(smem));
+      mbar_wait(k_full, 0, abort_flag, status, 0x4D01u);
+      for (int t = t0; t < t1; ++t) {
+        const uint32_t j = t - t0, st = j % ST, sb = j & 1;
+        mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D02u);
+        mbar_wait(s_empty + sb, ((j >> 1) & 1) ^ 1, abort_flag, status, 0x4D03u);
+        tc_fence_after();
+        const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + st * L::kTile));
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);
+          mma_ss(tmem + sb * 128, dk + off, dq + off, idesc, kk != 0);
+        }
+        tc_commit(s_full + sb);
+        tc_commit(q_empty + st);
+      }
+    }
+  } else {
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    const int first = first_row(key);
+    float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
+    for (int t = t0; t < t1; ++t) {
+      const uint32_t j = t - t0, st = j % ST, sb = j & 1;
+      mbar_wait(s_full + sb, (j >> 1) & 1, abort_flag, status, 0x4D04u);
+      mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D05u);     // row_stat
+      __syncwarp();
+      tc_fence_after();
+      const float4* stat = reinterpret_cast<const float4*>(smem + L::oStat + st * 1024);
+      const int hidden = first - t * 128;                 // rows of the tile that do not see this thread's key
+      const bool mask = __any_sync(0xffffffffu, hidden > 0);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint32_t z[32];
+        tmem_ld32(tmem + sb * 128 + lane_off + 32 * h, z);
+        tc_wait_ld();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+          const float4 s0 = stat[16 * h + i / 2], s1 = stat[16 * h + i / 2 + 1];
+          const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), make_float2(s0.x, s0.y), make_float2(s0.z, s0.w));
+          const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), make_float2(s1.x, s1.y), make_float2(s1.z, s1.w));
+          float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y)), p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
+          if (mask) {
+            const int at = 32 * h + i;
+            if (at < hidden) p0.x = 0.0f;
+            if (at + 1 < hidden) p0.y = 0.0f;
+            if (at + 2 < hidden) p1.x = 0.0f;
+            if (at + 3 < hidden) p1.y = 0.0f;
+          }
+          sum0 = __fadd2_rn(sum0, p0);
+          sum1 = __fadd2_rn(sum1, p1);
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(s_empty + sb);
+      mbar_arrive(q_empty + st);
+    }
+    if (key < len) {
+      const int64_t at = b * s.a.w_stride_b + head * s.a.w_stride_head + key;
+      s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 5) tmem_dealloc(tmem, 256);
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+constexpr size_t kRoundBytes = (size_t)2 << 30;      // dense copies of one round of sequences, one sequence at least
+
+struct Plan {
+  int rows_pad, keys_pad, round;                     // sequences of a round
+  size_t q16, k16, v16, q_factor, refs, row_stat, part_o, part_ml, desc, total;
+};
+Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d) {
+  Plan w;
+  const int D = c->head_dim;
+  const int64_t rows = (int64_t)d->tokens * (d->heads / c->kv_heads);
+  w.rows_pad = (int)spv_align_up((size_t)rows, kRowsUnit);
+  w.keys_pad = (int)spv_align_up((size_t)spv_kv_max_length(c, q), kKeys);
+  const size_t per = (size_t)c->kv_heads * D * 2 * (2 * (size_t)w.keys_pad + w.rows_pad);
+  size_t round = kRoundBytes / per;
+  // rows of the dense copies are numbered in 31 bits
+  const size_t most = (size_t)INT32_MAX / ((size_t)c->kv_heads * (w.keys_pad > w.rows_pad ? w.keys_pad : w.rows_pad));
+  if (round > most) round = most;
+  if (round < 1) round = 1;
+  if (round > (size_t)q->batch) round = q->batch;
+  w.round = (int)round;
+  const size_t pairs = round * c->kv_heads;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t x = at;
+    at += spv_align_up(bytes, 1024);
+    return x;
+  };
+  w.q16 = take(pairs * w.rows_pad * D * 2);
+  w.k16 = take(pairs * w.keys_pad * D * 2);
+  w.v16 = take(pairs * w.keys_pad * D * 2);
+  w.q_factor = take(pairs * w.rows_pad * sizeof(float));
+  w.refs = take(pairs * sizeof(float2));
+  w.row_stat = take(pairs * w.rows_pad * sizeof(float2));
+  w.part_o = take((size_t)kMaxSms * 2 * kRowsUnit * D * sizeof(float));
+  w.part_ml = take((size_t)kMaxSms * 2 * kRowsUnit * sizeof(float2));
+  w.desc = take(kMaxSms * sizeof(Desc));
+  w.total = at;
+  return w;
+}
+
+template <int FMT, int D>
+int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvAttnArgs& a, const Plan& w, char* base,
+            cudaStream_t stream) {
+  PromptArgs s;
+  s.a = a;
+  s.rows_pad = w.rows_pad;
+  s.keys_pad = w.keys_pad;
+  s.q16 = (uint16_t*)(base + w.q16);
+  s.k16 = (uint16_t*)(base + w.k16);
+  s.v16 = (uint16_t*)(base + w.v16);
+  s.q_factor = (float*)(base + w.q_factor);
+  s.refs = (float2*)(base + w.refs);
+  s.row_stat = (float2*)(base + w.row_stat);
+  s.part_o = (float*)(base + w.part_o);
+  s.part_ml = (float2*)(base + w.part_ml);
+  s.desc = (Desc*)(base + w.desc);
+  const uint64_t strides[1] = {(uint64_t)D * 2};
+  const uint32_t box[2] = {64, 128};
+  const uint64_t q_dims[2] = {(uint64_t)D, (uint64_t)w.round * view.kv_heads * w.rows_pad};
+  const uint64_t k_dims[2] = {(uint64_t)D, (uint64_t)w.round * view.kv_heads * w.keys_pad};
+  CUtensorMap mq, mk, mv;      // 16-bit elements, copied as they are
+  int32_t st = spv_make_tmap_bf16(ctx, &mq, s.q16, 2, q_dims, strides, box);
+  if (st == SPV_OK) st = spv_make_tmap_bf16(ctx, &mk, s.k16, 2, k_dims, strides, box);
+  if (st == SPV_OK) st = spv_make_tmap_bf16(ctx, &mv, s.v16, 2, k_dims, strides, box);
+  if (st != SPV_OK) return st;
+  constexpr int attend_bytes = AttendSmem<D>::kTotal + 1024, weigh_bytes = WeighSmem<D>::kTotal + 1024;
+  static_assert(attend_bytes <= 227 * 1024 && 2 * (weigh_bytes + 1024) <= 227 * 1024, "shared memory");
+  constexpr uint32_t bit = 1u << (30 + (D == 128));
+  if (!(ctx->kv_configured & bit)) {
+    SPV_CUDA_OK(cudaFuncSetAttribute(kv_prompt_attend<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, attend_bytes));
+    SPV_CUDA_OK(cudaFuncSetAttribute(kv_prompt_weigh<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, weigh_bytes));
+    ctx->kv_configured |= bit;
+  }
+  const int ctas = ctx->sm_count < kMaxSms ? ctx->sm_count : kMaxSms;
+  const int key_chunks = w.keys_pad / kPrepRows, row_chunks = w.rows_pad / kPrepRows;
+  int launches = 0;
+  for (int b0 = 0; b0 < seqs->batch; b0 += w.round) {
+    s.b0 = b0;
+    s.nb = seqs->batch - b0 < w.round ? seqs->batch - b0 : w.round;
+    kv_prompt_prepare<FMT, D><<<dim3(key_chunks + row_chunks, view.kv_heads, s.nb), kPrepThreads, 0, stream>>>(view, s, key_chunks);
+    kv_prompt_attend<D><<<ctas, kAttendThreads, attend_bytes, stream>>>(mq, mk, mv, view, s);
+    kv_prompt_join<D><<<dim3(ctas, kRowsUnit / 16), 256, 0, stream>>>(view, s, ctas);
+    launches += 3;
+    if (a.w_out) {
+      kv_prompt_weigh<D><<<dim3(w.keys_pad / kKeys, view.kv_heads, s.nb), kWeighThreads, weigh_bytes, stream>>>(mq, mk, view, s);
+      ++launches;
+    }
+  }
+  return spv_launch_ok(ctx, launches);
+}
+
+}  // namespace
+
+size_t spv_kv_prompt_workspace(const spv_kv_cache* cache, const spv_kv_seqs* seqs, const spv_kv_attn_desc* d) {
+  return plan(cache, seqs, d).total;
+}
+
+int32_t spv_kv_prompt_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_seqs* seqs, const spv_kv_attn_desc* d,
+                          const KvAttnArgs& a, void* workspace, cudaStream_t stream) {
+  const Plan w = plan(cache, seqs, d);
+  const KvView view = kv_view(ctx, cache, seqs);
+  char* base = (char*)workspace;
+  if (cache->format == SPV_KV_INT8)
+    return cache->head_dim == 64 ? run<SPV_KV_INT8, 64>(ctx, seqs, view, a, w, base, stream)
+                                 : run<SPV_KV_INT8, 128>(ctx, seqs, view, a, w, base, stream);
+  return cache->head_dim == 64 ? run<SPV_KV_E4M3, 64>(ctx, seqs, view, a, w, base, stream)
+                               : run<SPV_KV_E4M3, 128>(ctx, seqs, view, a, w, base, stream);
+}

@@ -280,7 +280,6 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
     return at < share.working ? share.begin(at) : total;
   });
   const Share share(scan->total, workers);
-  asm volatile("griddepcontrol.launch_dependents;");
   Walk walk;
   walk.before = scan->before[warp];
   walk.b = scan->b[warp];
@@ -710,7 +709,6 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
   for (int b = blockIdx.x; b < s.a.batch; b += gridDim.x)
     if (seq_key_tiles<kTile>(c, s.a, b) == 0) write_empty<D>(c, s.a, b);
   const int first = blockIdx.x * finish_workers(row_slots);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   const Stretch at = s.stretch[first];
   const Share share(at.total, workers);
   if (first >= share.working) return;
@@ -912,19 +910,10 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if (cache->format == SPV_KV_INT8) st = cache->head_dim == 64 ? go(I8(), D64()) : go(I8(), D128());
   else st = cache->head_dim == 64 ? go(E4(), D64()) : go(E4(), D128());
   if (st != SPV_OK) return st;
-  // the second kernel's launch overlaps the first; it waits on the device for the first to end
-  cudaLaunchConfig_t cfg = {};
   const int workers = ctas * warps_of(slots);
   const int64_t used = most < workers ? most : workers;
-  cfg.gridDim = dim3((unsigned)((used + finish_workers(slots) - 1) / finish_workers(slots)));
-  cfg.blockDim = dim3(kFinishThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  SPV_CUDA_OK(cache->head_dim == 64 ? cudaLaunchKernelEx(&cfg, kv_finish_kernel<64>, view, s, workers, slots)
-                                    : cudaLaunchKernelEx(&cfg, kv_finish_kernel<128>, view, s, workers, slots));
+  const unsigned blocks = (unsigned)((used + finish_workers(slots) - 1) / finish_workers(slots));
+  if (cache->head_dim == 64) kv_finish_kernel<64><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots);
+  else kv_finish_kernel<128><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots);
   return spv_launch_ok(ctx, 2);
 }

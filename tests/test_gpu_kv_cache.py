@@ -304,6 +304,16 @@ def test_attention_many_tiles_for_every_sm(ctx, fmt, dtype, dim, group, tokens):
     run_attention(ctx, rng, [9001, 40, 0, 7777, 3000, 1, 5000], tokens, None, 8 * group, 8, dim, 64, fmt, dtype, True)
 
 
+@pytest.mark.parametrize("fmt,dtype,dim,group,causal", [("int8", "bf16", 128, 4, True), ("e4m3", "fp16", 64, 3, False),
+                                                        ("e4m3", "bf16", 128, 1, True)])
+def test_attention_long_prompts(ctx, fmt, dtype, dim, group, causal):
+    """Units of rows and keys that are cut between SMs, more key tiles than are held at a time, a prompt that begins in
+    an empty cache, a padded one, and one without queries."""
+    rng = np.random.default_rng(dim * group)
+    run_attention(ctx, rng, [2900, 700, 0, 1333, 150, 2048], 700, [700, 700, 1, 0, 133, 389], 2 * group, 2, dim, 64, fmt, dtype,
+                  causal)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_attention_uneven_scales(ctx, fmt):
     """Blocks whose keys and values differ by many powers of two, an all-zero block, one far larger than the rest."""
