@@ -8,9 +8,12 @@
 //                        read by rows / 256 CTAs; converting it in each of them would cost more than half of the issue
 //                        slots that the softmax needs (1.4 instructions a code against 5 a score).
 //   kv_prompt_attend     one CTA per SM.  Units of 256 query rows x 128 keys form a line, and every CTA takes an equal
-//                        stretch of it.  Two row blocks of 128 take turns: while the eight warps of softmax work on one
-//                        block's scores (TMEM, a thread per row), the tensor cores do the other's S = Q K^T and
-//                        O += P V (P stays in TMEM, over its S).
+//                        stretch of it.  Eight warps of softmax have a row a thread, in two blocks of 128 rows; a block's
+//                        scores of 64 keys are in one of two TMEM buffers, so that S = Q K^T of the next 64 runs under
+//                        the softmax of these (P stays in TMEM, over its S).  A thread gets a tcgen05.mma issued every
+//                        118 cycles whatever its size: four threads issue, S and O of each block.  (Whole tiles of 128
+//                        keys in one buffer, two issuing threads: a block's chain of S, softmax and O was 6200 cycles a
+//                        tile, 208 us for 2 x 1501 tokens over 6001 slots, 32 heads of 128.)
 //   kv_prompt_join       units that were cut between CTAs.
 //   kv_prompt_weigh      weights: S^T = K Q^T by tiles of 128 keys, so that a key's scores are a thread's own and its
 //                        sum over the rows needs no other thread; 2^(z - lse) with the rows' lse from before.
@@ -266,7 +269,8 @@ __device__ __forceinline__ uint64_t smem_desc_parts(uint32_t saddr, uint32_t par
 }
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
-constexpr int kAttendThreads = 384;        // two warpgroups of softmax; producer, two issuers of products
+constexpr int kAttendThreads = 512;        // two warpgroups of softmax; producer, four issuers of products
+constexpr int kSub = 64;                   // keys whose scores are in a buffer
 template <int D>
 struct AttendSmem {
   static constexpr int kTile = 128 * D * 2;          // 128 rows of fp16: D / 64 parts of 128-byte rows
@@ -299,15 +303,15 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   uint64_t* k_empty = k_full + ST;
   uint64_t* v_full = k_empty + ST;
   uint64_t* v_empty = v_full + ST;
-  uint64_t* s_full = v_empty + ST;         // [2]
-  uint64_t* p_full = s_full + 2;           // [2]
-  uint64_t* o_full = p_full + 2;           // [2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 2);
+  uint64_t* s_full = v_empty + ST;         // [block][buffer]
+  uint64_t* p_full = s_full + 4;           // [block][buffer]
+  uint64_t* pv_done = p_full + 4;          // [block][buffer] the product with the buffer's P, and all before it, are done
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pv_done + 4);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   int* s_total = reinterpret_cast<int*>(tmem_slot + 2);
   int* s_before = s_total + 1;
   int* s_b = s_total + 2;
-  int* warp_sum = s_total + 4;             // [12]
+  int* warp_sum = s_total + 4;             // [16]
   uint32_t* status = c.status - 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -320,10 +324,10 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       mbar_init(v_full + i, 1);
       mbar_init(v_empty + i, 2);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 128);
-      mbar_init(o_full + i, 1);
+      mbar_init(pv_done + i, 1);
     }
     *abort_flag = 0u;
     mbar_fence_init();
@@ -424,12 +428,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
       }
     } else if (warp < 11) {
-      // ---- products of one row block
+      // ---- S = Q K^T of one block
       if (lane == 0) {
         const int x = warp - 9;
-        constexpr uint32_t idesc_s = idesc_f16(128, kKeys, false), idesc_o = idesc_f16(128, D, true);
-        const uint32_t t_s = tmem + x * 128, t_o = tmem + 256 + x * 128;
-        uint32_t kv = 0, pieces = 0, mine = 0;
+        constexpr uint32_t idesc = idesc_f16(128, kSub, false);
+        uint32_t kv = 0, pieces = 0, t = 0;              // t: scores buffers filled
         while (next_piece(c, s, walk, p)) {
           const int row0 = p.unit * kRowsUnit + x * 128;
           const int tiles = block_tiles(p.len, p.n, s.a.group, s.a.causal, row0, row0 + 128);
@@ -437,45 +440,68 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           ++pieces;
           const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + x * L::kTile));
           for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
-            const uint32_t st = kv % ST, ph = (kv / ST) & 1;
+            const uint32_t st = kv % ST;
+            mbar_wait(k_full + st, (kv / ST) & 1, abort_flag, status, 0x4C04u);
             if (kt >= tiles) {               // this block sees none of the tile
-              mbar_wait(k_full + st, ph, abort_flag, status, 0x4C04u);
               mbar_arrive(k_empty + st);
-              mbar_wait(v_full + st, ph, abort_flag, status, 0x4C05u);
+              continue;
+            }
+            const uint64_t dk = smem_desc_sw128(smem_u32(smem + L::oK + st * L::kTile));
+            for (int h = 0; h < 2; ++h, ++t) {
+              const uint32_t buf = t & 1;
+              if (t >= 2) mbar_wait(pv_done + 2 * x + buf, ((t >> 1) - 1) & 1, abort_flag, status, 0x4C05u);
+              tc_fence_after();
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);      // parts of 64 values are 16 KB apart
+                mma_ss(tmem + x * 128 + buf * kSub, dq + off, dk + off + h * 512, idesc, kk != 0);
+              }
+              tc_commit(s_full + 2 * x + buf);
+            }
+            tc_commit(k_empty + st);
+          }
+          tc_commit(q_empty);
+        }
+      }
+    } else if (warp < 13) {
+      // ---- O += P V of one block
+      if (lane == 0) {
+        const int x = warp - 11;
+        constexpr uint32_t idesc = idesc_f16(128, D, true);
+        uint32_t kv = 0, t = 0;
+        while (next_piece(c, s, walk, p)) {
+          const int row0 = p.unit * kRowsUnit + x * 128;
+          const int tiles = block_tiles(p.len, p.n, s.a.group, s.a.causal, row0, row0 + 128);
+          for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
+            const uint32_t st = kv % ST;
+            mbar_wait(v_full + st, (kv / ST) & 1, abort_flag, status, 0x4C06u);
+            if (kt >= tiles) {
               mbar_arrive(v_empty + st);
               continue;
             }
-            mbar_wait(k_full + st, ph, abort_flag, status, 0x4C06u);
-            tc_fence_after();
-            const uint64_t dk = smem_desc_sw128(smem_u32(smem + L::oK + st * L::kTile));
-#pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-              const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);      // parts of 64 are 16 KB apart
-              mma_ss(t_s, dq + off, dk + off, idesc_s, kk != 0);
-            }
-            tc_commit(s_full + x);
-            tc_commit(k_empty + st);
-            mbar_wait(v_full + st, ph, abort_flag, status, 0x4C07u);
-            mbar_wait(p_full + x, mine & 1, abort_flag, status, 0x4C08u);
-            tc_fence_after();
             const uint64_t dv = smem_desc_parts(smem_u32(smem + L::oV + st * L::kTile), 128 * 128);
+            for (int h = 0; h < 2; ++h, ++t) {
+              const uint32_t buf = t & 1;
+              mbar_wait(p_full + 2 * x + buf, (t >> 1) & 1, abort_flag, status, 0x4C07u);
+              tc_fence_after();
 #pragma unroll
-            for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(t_o, t_s + kk * 8, dv + (uint64_t)(kk * 128), idesc_o, (kt > p.kt0) | (kk != 0));
+              for (int kk = 0; kk < kSub / 16; ++kk)
+                mma_ts(tmem + 256 + x * 128, tmem + x * 128 + buf * kSub + kk * 8, dv + (uint64_t)((h * 4 + kk) * 128), idesc,
+                       (kt > p.kt0) | (h != 0) | (kk != 0));
+              tc_commit(pv_done + 2 * x + buf);
+            }
             tc_commit(v_empty + st);
-            ++mine;
           }
-          if (min(tiles, p.kt1) > p.kt0) tc_commit(o_full + x);
-          tc_commit(q_empty);
         }
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
     // ---- softmax: a thread per row
     const int x = warp >> 2, row_in = (warp & 3) * 32 + lane;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + x * 128 + lane_off, t_o = tmem + 256 + x * 128 + lane_off;
-    uint32_t mine = 0, outs = 0;
+    uint32_t sub = 0;                        // scores buffers used
     while (next_piece(c, s, walk, p)) {
       const int pair = p.b * c.kv_heads + p.head;
       const int block0 = p.unit * kRowsUnit + x * 128, row = block0 + row_in, rows = p.n * s.a.group;
@@ -485,77 +511,76 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const float f = real ? s.q_factor[(size_t)pair * s.rows_pad + row] * ref.x : 0.0f;
       const int end = real ? spv_kv_query_end(p.len, p.n, row / s.a.group, s.a.causal) : p.len;
       float m = kFloor, l = 0.0f;
-      for (int kt = p.kt0; kt < tiles; ++kt, ++mine) {
-        mbar_wait(s_full + x, mine & 1, abort_flag, status, 0x4C09u);
+      for (int t = 2 * p.kt0; t < 2 * tiles; ++t, ++sub) {
+        const uint32_t buf = sub & 1, at = t_s + buf * kSub;
+        mbar_wait(s_full + 2 * x + buf, (sub >> 1) & 1, abort_flag, status, 0x4C09u);
         __syncwarp();
         tc_fence_after();
-        uint32_t z[kKeys];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(t_s + 32 * i, z + 32 * i);
+        uint32_t z[kSub];
+        tmem_ld32(at, z);
+        tmem_ld32(at + 32, z + 32);
         tc_wait_ld();
-        const int see = end - kt * kKeys;
-        if (see < kKeys) {
+        const int see = end - t * kSub;
+        if (see < kSub) {
 #pragma unroll
-          for (int i = 0; i < kKeys; ++i)
+          for (int i = 0; i < kSub; ++i)
             if (i >= see) z[i] = 0xff800000u;
         }
         float t0 = -INFINITY, t1 = -INFINITY, t2 = -INFINITY, t3 = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kKeys; i += 8) {
+        for (int i = 0; i < kSub; i += 8) {
           t0 = max3(t0, __uint_as_float(z[i]), __uint_as_float(z[i + 1]));
           t1 = max3(t1, __uint_as_float(z[i + 2]), __uint_as_float(z[i + 3]));
           t2 = max3(t2, __uint_as_float(z[i + 4]), __uint_as_float(z[i + 5]));
           t3 = max3(t3, __uint_as_float(z[i + 6]), __uint_as_float(z[i + 7]));
         }
-        // the maximum is renewed only where it would grow by more than 2^8; every product before this S has completed,
-        // so the results may be rescaled at once
+        // the maximum is renewed only where it would grow by more than 2^8
         const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * f;
         const bool need = top > m + 8.0f;
         const float m_new = need ? top : m;
         const float alpha = need ? exp2_fast(m - m_new) : 1.0f;
-        if (__any_sync(0xffffffffu, need && l > 0.0f)) {
+        if (__any_sync(0xffffffffu, need && l > 0.0f)) {     // l > 0: the piece has a buffer before this one
+          mbar_wait(pv_done + 2 * x + ((sub - 1) & 1), ((sub - 1) >> 1) & 1, abort_flag, status, 0x4C0Au);
+          __syncwarp();
+          tc_fence_after();
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i) {
-            uint32_t o[16];
-            tmem_ld16(t_o + 16 * i, o);
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tmem_ld32(t_o + 32 * i, o);
             tc_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-            tmem_st16(t_o + 16 * i, o);
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(t_o + 32 * i, o);
           }
         }
         m = m_new;
         float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
         const float2 f2 = make_float2(f, f), nm = make_float2(-m, -m);
+        uint32_t pk[kSub / 2];
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t pk[16];
-#pragma unroll
-          for (int i = 0; i < 32; i += 4) {
-            const uint32_t* y = z + 32 * h + i;
-            const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(y[0]), __uint_as_float(y[1])), f2, nm);
-            const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(y[2]), __uint_as_float(y[3])), f2, nm);
-            const float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y));
-            const float2 p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
-            sum0 = __fadd2_rn(sum0, p0);
-            sum1 = __fadd2_rn(sum1, p1);
-            pk[i / 2] = kv_pack2<SPV_FP16>(p0.x, p0.y);
-            pk[i / 2 + 1] = kv_pack2<SPV_FP16>(p1.x, p1.y);
-          }
-          tmem_st16(t_s + 16 * h, pk);
+        for (int i = 0; i < kSub; i += 4) {
+          const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), f2, nm);
+          const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), f2, nm);
+          const float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y));
+          const float2 p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
+          sum0 = __fadd2_rn(sum0, p0);
+          sum1 = __fadd2_rn(sum1, p1);
+          pk[i / 2] = kv_pack2<SPV_FP16>(p0.x, p0.y);
+          pk[i / 2 + 1] = kv_pack2<SPV_FP16>(p1.x, p1.y);
         }
+        tmem_st32(at, pk);
         l = l * alpha + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
         tc_wait_st();
         tc_fence_before();
-        mbar_arrive(p_full + x);
+        mbar_arrive(p_full + 2 * x + buf);
       }
       // ---- results of the piece
       const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
       const size_t slot = ((size_t)(2 * blockIdx.x + (p.kt0 > 0 ? 0 : 1)) * kRowsUnit) + x * 128 + row_in;
       const bool any = tiles > p.kt0;        // uniform: the block saw a tile of the piece
       if (any) {
-        mbar_wait(o_full + x, outs & 1, abort_flag, status, 0x4C0Au);
-        ++outs;
+        mbar_wait(pv_done + 2 * x + ((sub - 1) & 1), ((sub - 1) >> 1) & 1, abort_flag, status, 0x4C0Bu);
+        __syncwarp();
         tc_fence_after();
       }
       const float inv = l > 0.0f ? ref.y / l : 0.0f;
@@ -658,7 +683,7 @@ __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const Prom
 }
 
 // ---- weights: grid (key tiles, key heads, sequences), two CTAs an SM ------------------------------------
-constexpr int kWeighThreads = 192;         // four warps of sums (a thread per key), producer, issuer
+constexpr int kWeighThreads = 320;         // eight warps of sums (two threads per key, half of the rows each), producer, issuer
 template <int D>
 struct WeighSmem {
   static constexpr int kTile = 128 * D * 2;
@@ -666,7 +691,8 @@ struct WeighSmem {
   static constexpr int oQ = kTile;
   static constexpr int oStat = oQ + kStages * kTile;       // row_stat of the tile, by pairs of rows: f, f', -lse, -lse'
   static constexpr int oBars = oStat + kStages * 128 * 8;
-  static constexpr int kTotal = oBars + 256;
+  static constexpr int oHalf = oBars + 256;                // sums of the second half of the rows
+  static constexpr int kTotal = oHalf + 512;
 };
 
 template <int D>
@@ -682,7 +708,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
   // rows that see a key: those from (key - (len - n)) * group on, where the mask is causal
   auto first_row = [&](int key) { return s.a.causal ? (int)max((int64_t)0, ((int64_t)key - len + n) * s.a.group) : 0; };
   const int t0 = min(first_row(key0), rows) / 128, t1 = (rows + 127) / 128;
-  const int key = key0 + threadIdx.x;
+  const int key = key0 + (threadIdx.x & 127);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::oBars);
@@ -699,16 +725,16 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
     mbar_init(k_full, 1);
     for (int i = 0; i < ST; ++i) {
       mbar_init(q_full + i, 2);
-      mbar_init(q_empty + i, 1 + 128);
+      mbar_init(q_empty + i, 1 + 256);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + i, 1);
-      mbar_init(s_empty + i, 128);
+      mbar_init(s_empty + i, 256);
     }
     *abort_flag = 0u;
     mbar_fence_init();
   }
-  if (warp == 5) {
+  if (warp == 9) {
     tmem_alloc(tmem_slot, 256);
     tmem_relinquish();
   }
@@ -716,7 +742,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  if (warp == 4) {
+  if (warp == 8) {
     if (lane == 0 && t0 < t1) {
       mbar_expect_tx(k_full, L::kTile);
       load_tile<D>(smem, &map_k, k_full, pair * s.keys_pad + key0);
@@ -739,7 +765,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
       if (lane == 0) mbar_arrive(q_full + st);
       __syncwarp();
     }
-  } else if (warp == 5) {
+  } else if (warp == 9) {
     if (lane == 0 && t0 < t1) {
       constexpr uint32_t idesc = idesc_f16(128, 128, false);
       const uint64_t dk = smem_desc_sw128(smem_u32(smem));
@@ -760,7 +786,8 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
       }
     }
   } else {
-    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const int half = warp >> 2;              // its rows of a tile: 64 half ..
     const int first = first_row(key);
     float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
     for (int t = t0; t < t1; ++t) {
@@ -773,7 +800,8 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
       const int hidden = first - t * 128;                 // rows of the tile that do not see this thread's key
       const bool mask = __any_sync(0xffffffffu, hidden > 0);
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
+      for (int g = 0; g < 2; ++g) {
+        const int h = 2 * half + g;
         uint32_t z[32];
         tmem_ld32(tmem + sb * 128 + lane_off + 32 * h, z);
         tc_wait_ld();
@@ -798,15 +826,19 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
       mbar_arrive(s_empty + sb);
       mbar_arrive(q_empty + st);
     }
-    if (key < len) {
+    float* other = reinterpret_cast<float*>(smem + L::oHalf);
+    const float sum = (sum0.x + sum0.y) + (sum1.x + sum1.y);
+    if (half) other[threadIdx.x & 127] = sum;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (!half && key < len) {
       const int64_t at = b * s.a.w_stride_b + head * s.a.w_stride_head + key;
-      s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
+      s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + (sum + other[threadIdx.x]);
     }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 5) tmem_dealloc(tmem, 256);
+  if (warp == 9) tmem_dealloc(tmem, 256);
 }
 
 // ---- host --------------------------------------------------------------------------------------------
