@@ -30,8 +30,10 @@ constexpr int kKeys = 128;
 constexpr int kMaxSms = 160;
 constexpr float kFloor = -1.0e30f;         // running maximum before the first key
 
-struct Desc {                              // last unit of a CTA's stretch
-  int total, b, head, unit, line, tiles, rows, n;
+struct alignas(16) Unit {                  // 256 query rows of a pair and the key tiles that they see
+  int b, head, unit;                       // b within the round
+  int line, tiles;                         // its tiles are [line, line + tiles) of the line
+  int len, n, pad;
 };
 
 struct PromptArgs {
@@ -46,7 +48,9 @@ struct PromptArgs {
   float2* row_stat;                        // [nb * kv_heads][rows_pad]: score factor, -lse (log2 domain)
   float* part_o;                           // [CTA][2][256][D]
   float2* part_ml;                         // [CTA][2][256]
-  Desc* desc;                              // [CTA]
+  Unit* units;                             // in the order of the line
+  int* head;                               // [0] tiles of the line, then for each CTA the units its stretch begins and ends in
+  int32_t ctas;
 };
 
 __device__ __forceinline__ int seq_len(const KvView& c, int b) { return spv_kv_clamp(__ldg(c.lengths + b), c.max_length); }
@@ -69,9 +73,127 @@ __device__ __forceinline__ float block_max(float x, float* tmp) {
   return x;
 }
 
-// grid (key chunks + query chunks of 64, key heads, sequences)
+// ---- the line of units -----------------------------------------------------------------------------
+// Key tiles of the rows [row0, row1): up to the last key that the last of them sees, one at least.
+__device__ __forceinline__ int block_tiles(int len, int n, int group, int causal, int row0, int row1) {
+  const int rows = n * group;
+  if (row0 >= rows) return 0;
+  const int end = spv_kv_query_end(len, n, (min(row1, rows) - 1) / group, causal);
+  return max(1, (end + kKeys - 1) / kKeys);
+}
+
+// Equal stretches of the line: the first `more` CTAs have per + 1 tiles, the others per.
+struct Share {
+  int working, per, more;
+  __device__ __forceinline__ Share(int total, int workers) {
+    working = min(total, workers);
+    per = working ? total / working : 0;
+    more = working ? total % working : 0;
+  }
+  __device__ __forceinline__ int begin(int worker) const { return worker * per + min(worker, more); }
+  __device__ __forceinline__ int owner(int t) const {
+    const int wide = more * (per + 1);
+    return t < wide ? t / (per + 1) : more + (t - wide) / per;
+  }
+};
+
+// One block: all units of the round in order, and where every CTA's stretch begins and ends.  A warp per sequence.
+__device__ void make_plan(const KvView& c, const PromptArgs& s) {
+  __shared__ int seq_units[kPrepThreads], seq_tiles[kPrepThreads];       // of the sequences of a batch of 256
+  __shared__ int base_units, base_tiles;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) base_units = base_tiles = 0;
+  for (int b0 = 0; b0 < s.nb; b0 += kPrepThreads) {
+    const int count = min(kPrepThreads, s.nb - b0);
+    for (int pass = 0; pass < 2; ++pass) {
+      // first the sums of every sequence, then, these summed up, its units
+      for (int i = warp; i < count; i += kPrepThreads / 32) {
+        const int b = b0 + i, len = seq_len(c, s.b0 + b), n = seq_queries(s.a, s.b0 + b);
+        const int units = (n * s.a.group + kRowsUnit - 1) / kRowsUnit;
+        const int first = pass ? seq_units[i] : 0, line0 = pass ? seq_tiles[i] : 0;
+        int per_head = 0;
+        for (int h = 0; h < (pass ? c.kv_heads : 1); ++h) {
+          int at = 0;
+          for (int u0 = 0; u0 < units; u0 += 32) {
+            const int u = u0 + lane;
+            const int t = u < units ? block_tiles(len, n, s.a.group, s.a.causal, u * kRowsUnit, (u + 1) * kRowsUnit) : 0;
+            int inc = t;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int x = __shfl_up_sync(0xffffffffu, inc, o);
+              if (lane >= o) inc += x;
+            }
+            if (pass && u < units)
+              s.units[first + h * units + u] = Unit{b, h, u, line0 + h * per_head + at + inc - t, t, len, n, 0};
+            at += __shfl_sync(0xffffffffu, inc, 31);
+          }
+          per_head = at;
+        }
+        if (!pass && lane == 0) {
+          seq_units[i] = units * c.kv_heads;
+          seq_tiles[i] = per_head * c.kv_heads;
+        }
+      }
+      __syncthreads();
+      if (!pass) {
+        if (threadIdx.x == 0) {
+          int u = base_units, t = base_tiles;
+          for (int i = 0; i < count; ++i) {
+            const int du = seq_units[i], dt = seq_tiles[i];
+            seq_units[i] = u;
+            seq_tiles[i] = t;
+            u += du;
+            t += dt;
+          }
+          base_units = u;
+          base_tiles = t;
+        }
+        __syncthreads();
+      }
+    }
+  }
+  __threadfence_block();
+  __syncthreads();
+  const int total = base_tiles, units = base_units;
+  const Share share(total, s.ctas);
+  if (threadIdx.x == 0) s.head[0] = total;
+  for (int i = threadIdx.x; i < units; i += kPrepThreads) {
+    const Unit u = s.units[i];
+    for (int w = share.owner(u.line); w <= share.owner(u.line + u.tiles - 1); ++w) {
+      if (share.begin(w) >= u.line) s.head[1 + 2 * w] = i;
+      if (share.begin(w + 1) <= u.line + u.tiles) s.head[2 + 2 * w] = i;
+    }
+  }
+}
+
+// The pieces of a CTA's stretch.
+struct Piece {
+  Unit u;
+  int kt0, kt1;                            // its key tiles of the unit
+};
+struct Walk {
+  int begin, end, next, last;              // tiles of the line; units
+};
+__device__ __forceinline__ Walk walk_of(const PromptArgs& s, const Share& share, int cta) {
+  Walk w{0, 0, 1, 0};
+  if (cta < share.working) w = Walk{share.begin(cta), share.begin(cta + 1), s.head[1 + 2 * cta], s.head[2 + 2 * cta]};
+  return w;
+}
+__device__ __forceinline__ bool next_piece(const PromptArgs& s, Walk& w, Piece& p) {
+  if (w.next > w.last) return false;
+  p.u = s.units[w.next++];
+  p.kt0 = max(0, w.begin - p.u.line);
+  p.kt1 = min(p.u.tiles, w.end - p.u.line);
+  return true;
+}
+
+// grid (key chunks + query chunks of 64 + one for the plan, key heads, sequences)
 template <int FMT, int D>
 __global__ void __launch_bounds__(kPrepThreads) kv_prompt_prepare(const KvView c, const PromptArgs s, int key_chunks) {
+  if (blockIdx.x == gridDim.x - 1) {
+    if (blockIdx.y == 0 && blockIdx.z == 0) make_plan(c, s);
+    return;
+  }
   const int head = blockIdx.y, bl = blockIdx.z, b = s.b0 + bl;
   const size_t pair = (size_t)bl * c.kv_heads + head;
   const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
@@ -163,97 +285,6 @@ __global__ void __launch_bounds__(kPrepThreads) kv_prompt_prepare(const KvView c
   }
 }
 
-// ---- the line of units -----------------------------------------------------------------------------
-// Key tiles of the unit whose rows are [unit * 256, ...): up to the last key that its last row sees, one at least.
-__device__ __forceinline__ int block_tiles(int len, int n, int group, int causal, int row0, int row1) {
-  const int rows = n * group;
-  if (row0 >= rows) return 0;
-  const int end = spv_kv_query_end(len, n, (min(row1, rows) - 1) / group, causal);
-  return max(1, (end + kKeys - 1) / kKeys);
-}
-__device__ __forceinline__ int unit_tiles(int len, int n, int group, int causal, int unit) {
-  return block_tiles(len, n, group, causal, unit * kRowsUnit, (unit + 1) * kRowsUnit);
-}
-__device__ __forceinline__ int seq_tiles(int len, int n, int group, int causal) {   // of one key head
-  const int units = (n * group + kRowsUnit - 1) / kRowsUnit;
-  if (!causal) return units * unit_tiles(len, n, group, 0, 0);
-  int sum = 0;
-  for (int u = 0; u < units; ++u) sum += unit_tiles(len, n, group, 1, u);
-  return sum;
-}
-
-struct Share {
-  int working, per, more;
-  __device__ __forceinline__ Share(int total, int workers) {
-    working = min(total, workers);
-    per = working ? total / working : 0;
-    more = working ? total % working : 0;
-  }
-  __device__ __forceinline__ int begin(int worker) const { return worker * per + min(worker, more); }
-  __device__ __forceinline__ int owner(int t) const {
-    const int wide = more * (per + 1);
-    return t < wide ? t / (per + 1) : more + (t - wide) / per;
-  }
-};
-
-struct Piece {
-  int b, head, unit, len, n;               // b within the round
-  int line, tiles, kt0, kt1;               // of the unit
-};
-struct Walk {
-  int pos, end, before, b;                 // before: tiles in front of sequence b
-  int head, unit, at;                      // unit that begins at `at` (-1: not yet looked up)
-};
-__device__ __forceinline__ bool next_piece(const KvView& c, const PromptArgs& s, Walk& w, Piece& p) {
-  if (w.pos >= w.end) return false;
-  for (;;) {
-    const int len = seq_len(c, s.b0 + w.b), n = seq_queries(s.a, s.b0 + w.b);
-    const int units = (n * s.a.group + kRowsUnit - 1) / kRowsUnit;
-    if (w.at < 0) {
-      const int per_head = n ? seq_tiles(len, n, s.a.group, s.a.causal) : 0;
-      if (w.pos >= w.before + c.kv_heads * per_head) {
-        w.before += c.kv_heads * per_head;
-        if (++w.b >= s.nb) return false;
-        continue;
-      }
-      w.head = (w.pos - w.before) / per_head;
-      w.unit = 0;
-      w.at = w.before + w.head * per_head;
-    }
-    while (w.unit < units) {
-      const int t = unit_tiles(len, n, s.a.group, s.a.causal, w.unit);
-      if (w.pos < w.at + t) {
-        p.b = w.b;
-        p.head = w.head;
-        p.unit = w.unit;
-        p.len = len;
-        p.n = n;
-        p.line = w.at;
-        p.tiles = t;
-        p.kt0 = w.pos - w.at;
-        p.kt1 = min(t, p.kt0 + w.end - w.pos);
-        w.pos += p.kt1 - p.kt0;
-        if (p.kt1 == t) {
-          w.at += t;
-          if (++w.unit == units) {
-            w.unit = 0;
-            if (++w.head == c.kv_heads) {
-              w.before = w.at;
-              ++w.b;
-              w.at = -1;
-              if (w.b >= s.nb) w.b = s.nb - 1, w.end = w.pos;
-            }
-          }
-        }
-        return true;
-      }
-      w.at += t;
-      ++w.unit;
-    }
-    return false;                            // not reached: every place of the line is in a unit
-  }
-}
-
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
   return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
@@ -308,10 +339,6 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   uint64_t* pv_done = p_full + 4;          // [block][buffer] the product with the buffer's P, and all before it, are done
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pv_done + 4);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  int* s_total = reinterpret_cast<int*>(tmem_slot + 2);
-  int* s_before = s_total + 1;
-  int* s_b = s_total + 2;
-  int* warp_sum = s_total + 4;             // [16]
   uint32_t* status = c.status - 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -336,59 +363,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     tmem_alloc(tmem_slot, 512);
     tmem_relinquish();
   }
-  // tiles of the sequences of this round, and where this CTA's stretch begins
-  {
-    const int per = (s.nb + kAttendThreads - 1) / kAttendThreads;
-    const int b0 = threadIdx.x * per, b1 = min(s.nb, b0 + per);
-    auto tiles = [&](int b) {
-      const int n = seq_queries(s.a, s.b0 + b);
-      return n ? c.kv_heads * seq_tiles(seq_len(c, s.b0 + b), n, s.a.group, s.a.causal) : 0;
-    };
-    int sum = 0;
-    for (int b = b0; b < b1; ++b) sum += tiles(b);
-    int inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += x;
-    }
-    if (lane == 31) warp_sum[warp] = inc;
-    __syncthreads();
-    int base = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kAttendThreads / 32; ++w) {
-      if (w < warp) base += warp_sum[w];
-      total += warp_sum[w];
-    }
-    const Share share(total, gridDim.x);
-    const int target = (int)blockIdx.x < share.working ? share.begin(blockIdx.x) : total;
-    int at = base + inc - sum;
-    if (target >= at && target < at + sum) {
-      int b = b0;
-      for (;; ++b) {
-        const int t = tiles(b);
-        if (target < at + t || b + 1 >= b1) break;
-        at += t;
-      }
-      *s_b = b;
-      *s_before = at;
-    }
-    if (threadIdx.x == 0) *s_total = total;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const Share share(*s_total, gridDim.x);
-  Walk walk;
-  walk.pos = walk.end = 0;
-  if ((int)blockIdx.x < share.working) {
-    walk.pos = share.begin(blockIdx.x);
-    walk.end = share.begin(blockIdx.x + 1);
-    walk.before = *s_before;
-    walk.b = *s_b;
-    walk.at = -1;
-  }
+  const Share share(s.head[0], gridDim.x);
+  Walk walk = walk_of(s, share, blockIdx.x);
   Piece p;
 
   if (warp >= 8) {
@@ -400,12 +380,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         tma_prefetch_desc(&map_k);
         tma_prefetch_desc(&map_v);
         uint32_t kv = 0, pieces = 0;
-        while (next_piece(c, s, walk, p)) {
-          const int pair = p.b * c.kv_heads + p.head;
+        while (next_piece(s, walk, p)) {
+          const int pair = p.u.b * c.kv_heads + p.u.head;
           if (pieces) mbar_wait(q_empty, (pieces - 1) & 1, abort_flag, status, 0x4C00u);
           mbar_expect_tx(q_full, 2 * L::kTile);
-          load_tile<D>(smem + L::oQ, &map_q, q_full, pair * s.rows_pad + p.unit * kRowsUnit);
-          load_tile<D>(smem + L::oQ + L::kTile, &map_q, q_full, pair * s.rows_pad + p.unit * kRowsUnit + 128);
+          load_tile<D>(smem + L::oQ, &map_q, q_full, pair * s.rows_pad + p.u.unit * kRowsUnit);
+          load_tile<D>(smem + L::oQ + L::kTile, &map_q, q_full, pair * s.rows_pad + p.u.unit * kRowsUnit + 128);
           ++pieces;
           for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
             const uint32_t st = kv % ST, ph = ((kv / ST) & 1) ^ 1;
@@ -433,9 +413,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const int x = warp - 9;
         constexpr uint32_t idesc = idesc_f16(128, kSub, false);
         uint32_t kv = 0, pieces = 0, t = 0;              // t: scores buffers filled
-        while (next_piece(c, s, walk, p)) {
-          const int row0 = p.unit * kRowsUnit + x * 128;
-          const int tiles = block_tiles(p.len, p.n, s.a.group, s.a.causal, row0, row0 + 128);
+        while (next_piece(s, walk, p)) {
+          const int row0 = p.u.unit * kRowsUnit + x * 128;
+          const int tiles = block_tiles(p.u.len, p.u.n, s.a.group, s.a.causal, row0, row0 + 128);
           mbar_wait(q_full, pieces & 1, abort_flag, status, 0x4C03u);
           ++pieces;
           const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + x * L::kTile));
@@ -469,9 +449,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const int x = warp - 11;
         constexpr uint32_t idesc = idesc_f16(128, D, true);
         uint32_t kv = 0, t = 0;
-        while (next_piece(c, s, walk, p)) {
-          const int row0 = p.unit * kRowsUnit + x * 128;
-          const int tiles = block_tiles(p.len, p.n, s.a.group, s.a.causal, row0, row0 + 128);
+        while (next_piece(s, walk, p)) {
+          const int row0 = p.u.unit * kRowsUnit + x * 128;
+          const int tiles = block_tiles(p.u.len, p.u.n, s.a.group, s.a.causal, row0, row0 + 128);
           for (int kt = p.kt0; kt < p.kt1; ++kt, ++kv) {
             const uint32_t st = kv % ST;
             mbar_wait(v_full + st, (kv / ST) & 1, abort_flag, status, 0x4C06u);
@@ -502,16 +482,27 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + x * 128 + lane_off, t_o = tmem + 256 + x * 128 + lane_off;
     uint32_t sub = 0;                        // scores buffers used
-    while (next_piece(c, s, walk, p)) {
-      const int pair = p.b * c.kv_heads + p.head;
-      const int block0 = p.unit * kRowsUnit + x * 128, row = block0 + row_in, rows = p.n * s.a.group;
-      const int tiles = min(p.kt1, block_tiles(p.len, p.n, s.a.group, s.a.causal, block0, block0 + 128));
+    // The blocks take turns with the exponentials, 64 a thread at a time: the special-function unit is then one warp's
+    // alone on every scheduler while the other block waits for its scores, reads them and looks for maxima.  (Left to
+    // themselves both come to it together and leave it idle together.)
+    auto my_turn = [&] { asm volatile("bar.sync %0, 256;" ::"r"(1 + x) : "memory"); };
+    auto others_turn = [&] { asm volatile("bar.arrive %0, 256;" ::"r"(2 - x) : "memory"); };
+    if (x == 1) others_turn();               // the first block begins
+    while (next_piece(s, walk, p)) {
+      const int pair = p.u.b * c.kv_heads + p.u.head;
+      const int block0 = p.u.unit * kRowsUnit + x * 128, row = block0 + row_in, rows = p.u.n * s.a.group;
+      const int tiles = min(p.kt1, block_tiles(p.u.len, p.u.n, s.a.group, s.a.causal, block0, block0 + 128));
       const bool real = row < rows;
       const float2 ref = s.refs[pair];
       const float f = real ? s.q_factor[(size_t)pair * s.rows_pad + row] * ref.x : 0.0f;
-      const int end = real ? spv_kv_query_end(p.len, p.n, row / s.a.group, s.a.causal) : p.len;
+      const int end = real ? spv_kv_query_end(p.u.len, p.u.n, row / s.a.group, s.a.causal) : p.u.len;
       float m = kFloor, l = 0.0f;
-      for (int t = 2 * p.kt0; t < 2 * tiles; ++t, ++sub) {
+      for (int t = 2 * p.kt0; t < 2 * p.kt1; ++t) {
+        if (t >= 2 * tiles) {                // this block sees none of the tile: its turn is over at once
+          my_turn();
+          others_turn();
+          continue;
+        }
         const uint32_t buf = sub & 1, at = t_s + buf * kSub;
         mbar_wait(s_full + 2 * x + buf, (sub >> 1) & 1, abort_flag, status, 0x4C09u);
         __syncwarp();
@@ -554,6 +545,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           }
         }
         m = m_new;
+        my_turn();
         float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
         const float2 f2 = make_float2(f, f), nm = make_float2(-m, -m);
         uint32_t pk[kSub / 2];
@@ -568,14 +560,16 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           pk[i / 2] = kv_pack2<SPV_FP16>(p0.x, p0.y);
           pk[i / 2 + 1] = kv_pack2<SPV_FP16>(p1.x, p1.y);
         }
+        others_turn();
         tmem_st32(at, pk);
         l = l * alpha + ((sum0.x + sum0.y) + (sum1.x + sum1.y));
         tc_wait_st();
         tc_fence_before();
         mbar_arrive(p_full + 2 * x + buf);
+        ++sub;
       }
       // ---- results of the piece
-      const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
+      const bool whole = p.kt0 == 0 && p.kt1 == p.u.tiles;
       const size_t slot = ((size_t)(2 * blockIdx.x + (p.kt0 > 0 ? 0 : 1)) * kRowsUnit) + x * 128 + row_in;
       const bool any = tiles > p.kt0;        // uniform: the block saw a tile of the piece
       if (any) {
@@ -584,8 +578,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         tc_fence_after();
       }
       const float inv = l > 0.0f ? ref.y / l : 0.0f;
-      const int i_q = row / s.a.group, h_q = p.head * s.a.group + row % s.a.group;
-      uint16_t* out = s.a.o + (s.b0 + p.b) * s.a.o_stride_b + i_q * s.a.o_stride_tok + h_q * s.a.o_stride_head;
+      const int i_q = row / s.a.group, h_q = p.u.head * s.a.group + row % s.a.group;
+      uint16_t* out = s.a.o + (s.b0 + p.u.b) * s.a.o_stride_b + i_q * s.a.o_stride_tok + h_q * s.a.o_stride_head;
       if (any) {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -616,14 +610,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         s.part_ml[slot] = make_float2(l > 0.0f ? m : -INFINITY, l);
       } else {
         const float lse = l > 0.0f ? m + log2f(l) : -INFINITY;
-        if (real && s.a.lse) s.a.lse[((size_t)(s.b0 + p.b) * s.a.tokens + i_q) * s.a.heads + h_q] = lse * 0.6931471805599453f;
+        if (real && s.a.lse) s.a.lse[((size_t)(s.b0 + p.u.b) * s.a.tokens + i_q) * s.a.heads + h_q] = lse * 0.6931471805599453f;
         s.row_stat[(size_t)pair * s.rows_pad + row] = real && l > 0.0f ? make_float2(f, -lse) : make_float2(0.0f, -INFINITY);
       }
-    }
-    if (threadIdx.x == 0) {
-      Desc d = {*s_total, 0, 0, 0, 0, 0, 0, 0};
-      if ((int)blockIdx.x < share.working) d = Desc{*s_total, p.b, p.head, p.unit, p.line, p.tiles, p.n * s.a.group, p.n};
-      s.desc[blockIdx.x] = d;
     }
   }
   tc_fence_before();
@@ -635,10 +624,10 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 // ---- units that were cut: grid (CTA, 16 rows) ---------------------------------------------------------
 template <int D>
 __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const PromptArgs s, int ctas) {
-  const Desc d = s.desc[blockIdx.x];
-  const Share share(d.total, ctas);
+  const Share share(s.head[0], ctas);
   if ((int)blockIdx.x >= share.working) return;
-  const int c0 = share.owner(d.line), c1 = share.owner(d.line + d.tiles - 1);
+  const Unit d = s.units[s.head[2 + 2 * blockIdx.x]];      // the last one that begins here
+  const int c0 = share.owner(d.line), c1 = share.owner(d.line + d.tiles - 1), rows = d.n * s.a.group;
   if (c0 != (int)blockIdx.x || c0 == c1) return;
   const int pair = d.b * c.kv_heads + d.head;
   const float2 ref = s.refs[pair];
@@ -664,7 +653,7 @@ __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const Prom
       }
     }
     const bool some = den > 0.0f || den != den;
-    const bool real = row < d.rows;
+    const bool real = row < rows;
     if (real) {
       const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
       const float inv = some ? ref.y / den : 0.0f;
@@ -846,7 +835,7 @@ constexpr size_t kRoundBytes = (size_t)2 << 30;      // dense copies of one roun
 
 struct Plan {
   int rows_pad, keys_pad, round;                     // sequences of a round
-  size_t q16, k16, v16, q_factor, refs, row_stat, part_o, part_ml, desc, total;
+  size_t q16, k16, v16, q_factor, refs, row_stat, part_o, part_ml, units, head, total;
 };
 Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d) {
   Plan w;
@@ -877,7 +866,8 @@ Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d
   w.row_stat = take(pairs * w.rows_pad * sizeof(float2));
   w.part_o = take((size_t)kMaxSms * 2 * kRowsUnit * D * sizeof(float));
   w.part_ml = take((size_t)kMaxSms * 2 * kRowsUnit * sizeof(float2));
-  w.desc = take(kMaxSms * sizeof(Desc));
+  w.units = take(pairs * (w.rows_pad / kRowsUnit) * sizeof(Unit));
+  w.head = take((1 + 2 * kMaxSms) * sizeof(int));
   w.total = at;
   return w;
 }
@@ -897,7 +887,8 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
   s.row_stat = (float2*)(base + w.row_stat);
   s.part_o = (float*)(base + w.part_o);
   s.part_ml = (float2*)(base + w.part_ml);
-  s.desc = (Desc*)(base + w.desc);
+  s.units = (Unit*)(base + w.units);
+  s.head = (int*)(base + w.head);
   const uint64_t strides[1] = {(uint64_t)D * 2};
   const uint32_t box[2] = {64, 128};
   const uint64_t q_dims[2] = {(uint64_t)D, (uint64_t)w.round * view.kv_heads * w.rows_pad};
@@ -916,12 +907,13 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
     ctx->kv_configured |= bit;
   }
   const int ctas = ctx->sm_count < kMaxSms ? ctx->sm_count : kMaxSms;
+  s.ctas = ctas;
   const int key_chunks = w.keys_pad / kPrepRows, row_chunks = w.rows_pad / kPrepRows;
   int launches = 0;
   for (int b0 = 0; b0 < seqs->batch; b0 += w.round) {
     s.b0 = b0;
     s.nb = seqs->batch - b0 < w.round ? seqs->batch - b0 : w.round;
-    kv_prompt_prepare<FMT, D><<<dim3(key_chunks + row_chunks, view.kv_heads, s.nb), kPrepThreads, 0, stream>>>(view, s, key_chunks);
+    kv_prompt_prepare<FMT, D><<<dim3(key_chunks + row_chunks + 1, view.kv_heads, s.nb), kPrepThreads, 0, stream>>>(view, s, key_chunks);
     kv_prompt_attend<D><<<ctas, kAttendThreads, attend_bytes, stream>>>(mq, mk, mv, view, s);
     kv_prompt_join<D><<<dim3(ctas, kRowsUnit / 16), 256, 0, stream>>>(view, s, ctas);
     launches += 3;
