@@ -4,7 +4,7 @@
 // weights 2 * head_dim and one exponential more (a row's weights are known only after its last key).
 //
 //   kv_prompt_prepare    the sequences' codes as dense fp16, keys and values scaled by one power of two of their sequence
-//                        and head, queries by one of their row: exact but for what lies 2^-24 below.  Every key tile is
+//                        and head, queries by one of their 128 rows: exact but for what lies 2^-24 below.  Every key tile is
 //                        read by rows / 256 CTAs; converting it in each of them would cost more than half of the issue
 //                        slots that the softmax needs (1.4 instructions a code against 5 a score).
 //   kv_prompt_attend     one CTA per SM.  Units of 256 query rows x 128 keys form a line, and every CTA takes an equal
@@ -43,9 +43,9 @@ struct PromptArgs {
   uint16_t* q16;                           // [nb * kv_heads][rows_pad][D]
   uint16_t* k16;                           // [nb * kv_heads][keys_pad][D]
   uint16_t* v16;
-  float* q_factor;                         // [nb * kv_heads][rows_pad]: softmax scale, log2 e and the row's power of two
+  float* q_factor;                         // [nb * kv_heads][rows_pad / 128]: softmax scale, log2 e and the rows' power of two
   float2* refs;                            // [nb * kv_heads]: units of the keys and of the values
-  float2* row_stat;                        // [nb * kv_heads][rows_pad]: score factor, -lse (log2 domain)
+  float* row_stat;                         // [nb * kv_heads][rows_pad]: -lse (log2 domain)
   float* part_o;                           // [CTA][2][256][D]
   float2* part_ml;                         // [CTA][2][256]
   Unit* units;                             // in the order of the line
@@ -61,7 +61,7 @@ __device__ __forceinline__ int padded_keys(int len) { return max(kKeys, (len + k
 
 // ---- dense copies --------------------------------------------------------------------------------
 constexpr int kPrepThreads = 256;
-constexpr int kPrepRows = 64;
+constexpr int kPrepRows = 128;             // keys or query rows of a block
 
 __device__ __forceinline__ float block_max(float x, float* tmp) {
 #pragma unroll
@@ -187,7 +187,7 @@ __device__ __forceinline__ bool next_piece(const PromptArgs& s, Walk& w, Piece& 
   return true;
 }
 
-// grid (key chunks + query chunks of 64 + one for the plan, key heads, sequences)
+// grid (key chunks + query chunks of 128 + one for the plan, key heads, sequences)
 template <int FMT, int D>
 __global__ void __launch_bounds__(kPrepThreads) kv_prompt_prepare(const KvView c, const PromptArgs s, int key_chunks) {
   if (blockIdx.x == gridDim.x - 1) {
@@ -251,38 +251,51 @@ __global__ void __launch_bounds__(kPrepThreads) kv_prompt_prepare(const KvView c
     }
     return;
   }
-  // queries: a warp per row
-  const int rows = n * s.a.group, row_end = (rows + kRowsUnit - 1) / kRowsUnit * kRowsUnit;
+  // queries: 128 rows share a power of two, that of their largest finite value (the weights' kernel then has one score
+  // factor a tile); a row 2^17 below the largest still has every bit of its own largest values
+  const int rows = n * s.a.group;
   const int row0 = ((int)blockIdx.x - key_chunks) * kPrepRows;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int kPer = D / 32;
-  for (int row = row0 + warp; row < min(row0 + kPrepRows, row_end); row += kPrepThreads / 32) {
-    uint32_t w[kPer / 2];
+  if (row0 >= (rows + kRowsUnit - 1) / kRowsUnit * kRowsUnit) return;
+  __shared__ float tile_max[kPrepThreads / 32];
+  constexpr int kVecRow = D / 8, kMine = kPrepRows * kVecRow / kPrepThreads;
+  uint4 x[kMine];
+  uint32_t big = 0;
 #pragma unroll
-    for (int e = 0; e < kPer / 2; ++e) w[e] = 0u;
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kPrepThreads, row = row0 + v / kVecRow;
+    x[i] = make_uint4(0u, 0u, 0u, 0u);
     if (row < rows) {
-      const int i = row / s.a.group, h = head * s.a.group + row % s.a.group;
-      const uint16_t* src = s.a.q + b * s.a.q_stride_b + i * s.a.q_stride_tok + h * s.a.q_stride_head + lane * kPer;
-#pragma unroll
-      for (int e = 0; e < kPer / 2; ++e) w[e] = __ldg(reinterpret_cast<const uint32_t*>(src) + e);
+      const int q = row / s.a.group, h = head * s.a.group + row % s.a.group;
+      x[i] = __ldg(reinterpret_cast<const uint4*>(s.a.q + b * s.a.q_stride_b + q * s.a.q_stride_tok + h * s.a.q_stride_head) + v % kVecRow);
     }
-    float x[kPer];
-    uint32_t big = 0;
-#pragma unroll
-    for (int e = 0; e < kPer / 2; ++e) {
-      const float2 f = s.a.dtype == SPV_BF16 ? kv_unpack2<SPV_BF16>(w[e]) : kv_unpack2<SPV_FP16>(w[e]);
-      x[2 * e] = f.x;
-      x[2 * e + 1] = f.y;
-      big = max(big, max(__float_as_uint(f.x) & 0x7FFFFFFFu, __float_as_uint(f.y) & 0x7FFFFFFFu));
-    }
-    big = __reduce_max_sync(0xffffffffu, big);
-    const int ex = max((int)(big >> 23) - 127, -100);
-    const float up = kv_pow2(14 - ex);
-    uint32_t* dst = reinterpret_cast<uint32_t*>(s.q16 + (pair * s.rows_pad + row) * D + lane * kPer);
-#pragma unroll
-    for (int e = 0; e < kPer / 2; ++e) dst[e] = kv_pack2<SPV_FP16>(x[2 * e] * up, x[2 * e + 1] * up);
-    if (lane == 0) s.q_factor[pair * s.rows_pad + row] = s.a.scale * 1.4426950408889634f * kv_pow2(ex - 14);
   }
+  auto value = [&](uint32_t u) { return s.a.dtype == SPV_BF16 ? kv_unpack2<SPV_BF16>(u) : kv_unpack2<SPV_FP16>(u); };
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = value(w[j]);
+      const uint32_t p = __float_as_uint(f.x) & 0x7FFFFFFFu, q = __float_as_uint(f.y) & 0x7FFFFFFFu;
+      big = max(big, max(p < 0x7F800000u ? p : 0u, q < 0x7F800000u ? q : 0u));
+    }
+  }
+  big = __float_as_uint(block_max(__uint_as_float(big), tile_max));
+  const int ex = max((int)(big >> 23) - 127, -100);
+  const float up = kv_pow2(14 - ex);
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kPrepThreads, row = row0 + v / kVecRow;
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    uint32_t u[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = value(w[j]);
+      u[j] = kv_pack2<SPV_FP16>(f.x * up, f.y * up);
+    }
+    *(reinterpret_cast<uint4*>(s.q16 + (pair * s.rows_pad + row) * D) + v % kVecRow) = make_uint4(u[0], u[1], u[2], u[3]);
+  }
+  if (threadIdx.x == 0) s.q_factor[(pair * s.rows_pad + row0) / kPrepRows] = s.a.scale * 1.4426950408889634f * kv_pow2(ex - 14);
 }
 
 __host__ __device__ constexpr uint32_t idesc_f16(int m, int n, bool b_mn_major) {
@@ -494,7 +507,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const int tiles = min(p.kt1, block_tiles(p.u.len, p.u.n, s.a.group, s.a.causal, block0, block0 + 128));
       const bool real = row < rows;
       const float2 ref = s.refs[pair];
-      const float f = real ? s.q_factor[(size_t)pair * s.rows_pad + row] * ref.x : 0.0f;
+      const float f = s.q_factor[((size_t)pair * s.rows_pad + block0) / 128] * ref.x;
       const int end = real ? spv_kv_query_end(p.u.len, p.u.n, row / s.a.group, s.a.causal) : p.u.len;
       float m = kFloor, l = 0.0f;
       for (int t = 2 * p.kt0; t < 2 * p.kt1; ++t) {
@@ -609,9 +622,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       if (!whole) {
         s.part_ml[slot] = make_float2(l > 0.0f ? m : -INFINITY, l);
       } else {
-        const float lse = l > 0.0f ? m + log2f(l) : -INFINITY;
+        const float lse = l > 0.0f || l != l ? m + log2f(l) : -INFINITY;
         if (real && s.a.lse) s.a.lse[((size_t)(s.b0 + p.u.b) * s.a.tokens + i_q) * s.a.heads + h_q] = lse * 0.6931471805599453f;
-        s.row_stat[(size_t)pair * s.rows_pad + row] = real && l > 0.0f ? make_float2(f, -lse) : make_float2(0.0f, -INFINITY);
+        s.row_stat[(size_t)pair * s.rows_pad + row] = real && (l > 0.0f || l != l) ? -lse : -INFINITY;
       }
     }
   }
@@ -665,8 +678,7 @@ __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const Prom
         s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
     }
     if (col == 0) {
-      const size_t at = (size_t)pair * s.rows_pad + row;
-      s.row_stat[at] = real && some ? make_float2(s.q_factor[at] * ref.x, -(top + log2f(den))) : make_float2(0.0f, -INFINITY);
+      s.row_stat[(size_t)pair * s.rows_pad + row] = real && some ? -(top + log2f(den)) : -INFINITY;
     }
   }
 }
@@ -678,8 +690,8 @@ struct WeighSmem {
   static constexpr int kTile = 128 * D * 2;
   static constexpr int kStages = 2;
   static constexpr int oQ = kTile;
-  static constexpr int oStat = oQ + kStages * kTile;       // row_stat of the tile, by pairs of rows: f, f', -lse, -lse'
-  static constexpr int oBars = oStat + kStages * 128 * 8;
+  static constexpr int oStat = oQ + kStages * kTile;       // -lse of the tile's rows
+  static constexpr int oBars = oStat + kStages * 128 * 4;
   static constexpr int oHalf = oBars + 256;                // sums of the second half of the rows
   static constexpr int kTotal = oHalf + 512;
 };
@@ -743,13 +755,8 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
         mbar_expect_tx(q_full + st, L::kTile);
         load_tile<D>(smem + L::oQ + st * L::kTile, &map_q, q_full + st, pair * s.rows_pad + t * 128);
       }
-      float4* stat = reinterpret_cast<float4*>(smem + L::oStat + st * 1024);
-      const float4* src = reinterpret_cast<const float4*>(s.row_stat + (size_t)pair * s.rows_pad + t * 128);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float4 v = src[lane + 32 * i];
-        stat[lane + 32 * i] = make_float4(v.x, v.z, v.y, v.w);
-      }
+      reinterpret_cast<float4*>(smem + L::oStat + st * 512)[lane] =
+          reinterpret_cast<const float4*>(s.row_stat + (size_t)pair * s.rows_pad + t * 128)[lane];
       __syncwarp();
       if (lane == 0) mbar_arrive(q_full + st);
       __syncwarp();
@@ -778,6 +785,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const int half = warp >> 2;              // its rows of a tile: 64 half ..
     const int first = first_row(key);
+    const float unit = t0 < t1 ? s.refs[pair].x : 0.0f;
     float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
     for (int t = t0; t < t1; ++t) {
       const uint32_t j = t - t0, st = j % ST, sb = j & 1;
@@ -785,7 +793,9 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
       mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D05u);     // row_stat
       __syncwarp();
       tc_fence_after();
-      const float4* stat = reinterpret_cast<const float4*>(smem + L::oStat + st * 1024);
+      const float4* stat = reinterpret_cast<const float4*>(smem + L::oStat + st * 512);
+      const float f = s.q_factor[(size_t)pair * (s.rows_pad / 128) + t] * unit;
+      const float2 f2 = make_float2(f, f);
       const int hidden = first - t * 128;                 // rows of the tile that do not see this thread's key
       const bool mask = __any_sync(0xffffffffu, hidden > 0);
 #pragma unroll
@@ -796,9 +806,9 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
         tc_wait_ld();
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-          const float4 s0 = stat[16 * h + i / 2], s1 = stat[16 * h + i / 2 + 1];
-          const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), make_float2(s0.x, s0.y), make_float2(s0.z, s0.w));
-          const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), make_float2(s1.x, s1.y), make_float2(s1.z, s1.w));
+          const float4 nl = stat[8 * h + i / 4];
+          const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), f2, make_float2(nl.x, nl.y));
+          const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), f2, make_float2(nl.z, nl.w));
           float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y)), p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
           if (mask) {
             const int at = 32 * h + i;
@@ -861,9 +871,9 @@ Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d
   w.q16 = take(pairs * w.rows_pad * D * 2);
   w.k16 = take(pairs * w.keys_pad * D * 2);
   w.v16 = take(pairs * w.keys_pad * D * 2);
-  w.q_factor = take(pairs * w.rows_pad * sizeof(float));
+  w.q_factor = take(pairs * (w.rows_pad / 128) * sizeof(float));
   w.refs = take(pairs * sizeof(float2));
-  w.row_stat = take(pairs * w.rows_pad * sizeof(float2));
+  w.row_stat = take(pairs * w.rows_pad * sizeof(float));
   w.part_o = take((size_t)kMaxSms * 2 * kRowsUnit * D * sizeof(float));
   w.part_ml = take((size_t)kMaxSms * 2 * kRowsUnit * sizeof(float2));
   w.units = take(pairs * (w.rows_pad / kRowsUnit) * sizeof(Unit));
@@ -884,7 +894,7 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
   s.v16 = (uint16_t*)(base + w.v16);
   s.q_factor = (float*)(base + w.q_factor);
   s.refs = (float2*)(base + w.refs);
-  s.row_stat = (float2*)(base + w.row_stat);
+  s.row_stat = (float*)(base + w.row_stat);
   s.part_o = (float*)(base + w.part_o);
   s.part_ml = (float2*)(base + w.part_ml);
   s.units = (Unit*)(base + w.units);
