@@ -65,7 +65,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 }
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
-  asm volatile("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
