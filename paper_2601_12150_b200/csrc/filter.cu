@@ -14,7 +14,6 @@
 
 namespace {
 
-using spv::block_scan2;
 using spv::kSelThreads;
 using spv::rank_key;
 constexpr int kSelItems = 4;
@@ -63,6 +62,38 @@ __global__ void __launch_bounds__(256) filter_mean_key_logits(const float* __res
   const int pos = cur_pos ? __ldg(cur_pos + (size_t)b * n_cur + t) : t;
   mean_ws[(size_t)b * npad + pos] = mean;
   key_ws[(size_t)b * npad + pos] = rank_key(mean);
+}
+
+// Block-wide exclusive scan of two counters; returns this thread's exclusive prefixes and the
+// block totals.  Called by all kSelThreads threads.
+__device__ __forceinline__ void block_scan2(int a, int b, int& ea, int& eb, int& ta, int& tb, int (*warp_tot)[2]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int ia = a, ib = b;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    int na = __shfl_up_sync(0xffffffffu, ia, o), nb = __shfl_up_sync(0xffffffffu, ib, o);
+    if (lane >= o) { ia += na; ib += nb; }
+  }
+  if (lane == 31) { warp_tot[warp][0] = ia; warp_tot[warp][1] = ib; }
+  __syncthreads();
+  if (warp == 0) {
+    int wa = warp_tot[lane][0], wb = warp_tot[lane][1];
+    int sa = wa, sb = wb;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      int na = __shfl_up_sync(0xffffffffu, sa, o), nb = __shfl_up_sync(0xffffffffu, sb, o);
+      if (lane >= o) { sa += na; sb += nb; }
+    }
+    warp_tot[lane][0] = sa - wa;   // exclusive warp offsets
+    warp_tot[lane][1] = sb - wb;
+    if (lane == 31) { warp_tot[32][0] = sa; warp_tot[32][1] = sb; }
+  }
+  __syncthreads();
+  ea = warp_tot[warp][0] + ia - a;
+  eb = warp_tot[warp][1] + ib - b;
+  ta = warp_tot[32][0];
+  tb = warp_tot[32][1];
+  __syncthreads();
 }
 
 __global__ void __launch_bounds__(kSelThreads) filter_select(const uint32_t* __restrict__ key_ws, int n_patch,

@@ -53,28 +53,38 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, AppendArg
   const uint16_t* src = a.src[which] + b * a.stride_b + (int64_t)(lo - len) * a.stride_tok + head * a.stride_head;
   const int nvec = (hi - lo) * kVecRow;
   uint4 x[kMaxVec];
-  uint32_t big = 0;
-  bool odd = false;
 #pragma unroll
   for (int i = 0; i < kMaxVec; ++i) {
     const int v = threadIdx.x + i * kThreads;
-    if (v < nvec) x[i] = __ldg(reinterpret_cast<const uint4*>(src + (v / kVecRow) * a.stride_tok) + v % kVecRow);
+    x[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (v < nvec) x[i] = __ldcs(reinterpret_cast<const uint4*>(src + (v / kVecRow) * a.stride_tok) + v % kVecRow);
   }
+  uint32_t top = 0;                                       // magnitudes, two 16-bit lanes
 #pragma unroll
   for (int i = 0; i < kMaxVec; ++i) {
-    if (threadIdx.x + i * kThreads < nvec) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = __vmaxu2(top, w[j] & 0x7FFF7FFFu);
+  }
+  constexpr uint32_t kInf = DT == SPV_BF16 ? 0x7F80u : 0x7C00u;
+  uint32_t big = block_max(max(top & 0xFFFFu, top >> 16), warp_max);
+  const bool odd = big >= kInf;                           // infinities or NaN among them: the largest of the others
+  if (odd) {
+    if (threadIdx.x == 0) kv_fault(c.status, SPV_SITE_KV_VALUE);
+    uint32_t fine = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxVec; ++i) {
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float2 f = kv_unpack2<DT>(w[j]);
-        const uint32_t p = __float_as_uint(f.x) & 0x7FFFFFFFu, q = __float_as_uint(f.y) & 0x7FFFFFFFu;
-        odd |= p >= 0x7F800000u || q >= 0x7F800000u;
-        big = max(big, max(p < 0x7F800000u ? p : 0u, q < 0x7F800000u ? q : 0u));
+        const uint32_t p = w[j] & 0x7FFFu, q = w[j] >> 16 & 0x7FFFu;
+        fine = max(fine, max(p < kInf ? p : 0u, q < kInf ? q : 0u));
       }
     }
+    __syncthreads();                                      // warp_max is read no more
+    big = block_max(fine, warp_max);
   }
-  if (odd) kv_fault(c.status, SPV_SITE_KV_VALUE);
-  big = block_max(big, warp_max);
+  big = __float_as_uint(kv_unpack2<DT>(big).x);
   float* scale_at = const_cast<float*>(which ? c.v_scale : c.k_scale) + (size_t)page * c.kv_heads + head;
   uint8_t* codes = const_cast<uint8_t*>(which ? c.v : c.k) + ((size_t)page * c.kv_heads + head) * a.block * D;
   float scale = kv_pow2(kv_exponent<FMT>(big));
@@ -87,17 +97,15 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, AppendArg
       const float f = old / scale;
       for (int v = threadIdx.x; v < held * (D / 16); v += kThreads) {
         uint4* at = reinterpret_cast<uint4*>(codes) + v;
-        uint4 t = *at;
-        uint32_t* w = &t.x;
+        const uint4 t = *at;
+        uint32_t w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float y[4];
           kv_decode4<FMT>(w[j], y);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] *= f;
-          w[j] = kv_encode4<FMT>(y);
+          w[j] = kv_encode4_finite<FMT>(y, f);
         }
-        *at = t;
+        *at = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
@@ -111,8 +119,13 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, AppendArg
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float2 p = kv_unpack2<DT>(w[2 * j]), q = kv_unpack2<DT>(w[2 * j + 1]);
-        const float y[4] = {p.x * inv, p.y * inv, q.x * inv, q.y * inv};
-        out[j] = kv_encode4<FMT>(y);
+        const float y[4] = {p.x, p.y, q.x, q.y};
+        if (odd) {
+          const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+          out[j] = kv_encode4<FMT>(z);
+        } else {
+          out[j] = kv_encode4_finite<FMT>(y, inv);
+        }
       }
       *reinterpret_cast<uint2*>(codes + (size_t)(held + v / kVecRow) * D + (v % kVecRow) * 8) = make_uint2(out[0], out[1]);
     }
@@ -206,12 +219,20 @@ struct EvictArgs {
   float* dst_vs;
 };
 
+// One CTA per (sequence, head).  Radix select with digits of 12, 10 and 10 bits (the first digit has three bits of the
+// significand: weights of one sequence share few exponents, and their counts would all meet in a few places), then the
+// survivors' places from ballots.  Up to 16384 keys stay in registers; longer rows are read again in every pass.
+constexpr int kSelItems = 16;
+constexpr int kSelTile = kSelItems * kSelThreads;
+
 __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictArgs a) {
-  __shared__ int hist[256];
-  __shared__ int warp_tot[33][2];
+  __shared__ int hist[4096];
+  __shared__ int2 counts[kSelItems * 32];       // of each item and warp: keys above the threshold, keys equal to it
+  __shared__ int warp_tot[32];
+  __shared__ int2 warp_tot2[32];
   __shared__ uint32_t s_prefix;
   __shared__ int s_remaining;
-  const int head = blockIdx.x, b = blockIdx.y;
+  const int head = blockIdx.x, b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
   const int n = min(len, a.budget);
   int32_t* kout = a.kept + ((size_t)b * c.kv_heads + head) * a.budget;
@@ -221,7 +242,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
     for (int t = threadIdx.x; t < n; t += kSelThreads) kout[t] = t;
     return;
   }
-  // the protected ends, then the k largest of the slots between them
+  // the protected ends, then the k largest of the m slots between them
   for (int t = threadIdx.x; t < a.keep_first; t += kSelThreads) kout[t] = t;
   for (int t = threadIdx.x; t < a.keep_last; t += kSelThreads) kout[n - a.keep_last + t] = len - a.keep_last + t;
   const int k = n - a.keep_first - a.keep_last;
@@ -229,55 +250,96 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
   if (k == 0) return;
   const float* w = a.weights + b * a.w_stride_b + head * a.w_stride_head + a.keep_first;
   kout += a.keep_first;
+  uint32_t key[kSelItems];
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < kSelItems; ++i) {
+      const int j = tile + i * kSelThreads + threadIdx.x;
+      key[i] = j < m ? rank_key(__ldg(w + j)) : 0u;
+    }
+  };
+  load(0);
   if (threadIdx.x == 0) { s_prefix = 0u; s_remaining = k; }
-  for (int pass = 0; pass < 4; ++pass) {
-    const int shift = 24 - 8 * pass;
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 20 : (pass == 1 ? 10 : 0), bins = pass == 0 ? 4096 : 1024;
+    for (int i = threadIdx.x; i < bins; i += kSelThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t prefix = s_prefix;
-    const uint32_t himask = pass == 0 ? 0u : (0xFFFFFFFFu << (shift + 8));
-    for (int i = threadIdx.x; i < m; i += kSelThreads) {
-      const uint32_t e = rank_key(__ldg(w + i));
-      if ((e & himask) == prefix) atomicAdd(&hist[(e >> shift) & 255u], 1);
+    const uint32_t himask = pass == 0 ? 0u : (pass == 1 ? 0xFFF00000u : 0xFFFFFC00u);
+    for (int tile = 0; tile < m; tile += kSelTile) {
+      if (m > kSelTile) load(tile);
+#pragma unroll
+      for (int i = 0; i < kSelItems; ++i)
+        if (tile + i * kSelThreads + (int)threadIdx.x < m && (key[i] & himask) == prefix)
+          atomicAdd(&hist[key[i] >> shift & (bins - 1)], 1);
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-      int rem = s_remaining, bin = 255;
-      for (; bin > 0; --bin) {
-        if (hist[bin] >= rem) break;
-        rem -= hist[bin];
-      }
-      s_prefix = prefix | ((uint32_t)bin << shift);
-      s_remaining = rem;
+    // the bin of the k-th largest: thread t sums the bins from the top down, `per` of them
+    const int per = bins / kSelThreads, remaining = s_remaining;
+    int own[4], sum = 0;
+    for (int i = 0; i < per; ++i) sum += own[i] = hist[bins - 1 - (threadIdx.x * per + i)];
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    if (lane == 31) warp_tot[warp] = inc;
+    __syncthreads();
+    int above = inc - sum;
+    {
+      const int x = warp_tot[lane];
+      const int before = lane < warp ? x : 0;
+      above += __reduce_add_sync(0xffffffffu, before);
+    }
+    if (above < remaining && above + sum >= remaining) {
+      int i = 0;
+      while (above + own[i] < remaining) above += own[i++];
+      s_prefix = prefix | (uint32_t)(bins - 1 - (threadIdx.x * per + i)) << shift;
+      s_remaining = remaining - above;
     }
     __syncthreads();
   }
   const uint32_t thr = s_prefix;     // k-th largest key
   const int need_eq = s_remaining;   // how many keys equal to it stay (lowest slots first)
   int base_gt = 0, base_eq = 0;
-  for (int tile0 = 0; tile0 < m; tile0 += 4 * kSelThreads) {
-    const int j0 = tile0 + 4 * threadIdx.x;
-    uint32_t e[4];
-    int gt = 0, eq = 0;
+  for (int tile = 0; tile < m; tile += kSelTile) {
+    if (m > kSelTile) load(tile);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const bool valid = j0 + t < m;
-      e[t] = valid ? rank_key(__ldg(w + j0 + t)) : 0u;
-      gt += valid && e[t] > thr ? 1 : 0;
-      eq += valid && e[t] == thr ? 1 : 0;
+    for (int i = 0; i < kSelItems; ++i) {
+      const bool valid = tile + i * kSelThreads + (int)threadIdx.x < m;
+      const uint32_t gt = __ballot_sync(0xffffffffu, valid && key[i] > thr), eq = __ballot_sync(0xffffffffu, valid && key[i] == thr);
+      if (lane == 0) counts[i * 32 + warp] = make_int2(__popc(gt), __popc(eq));
     }
-    int egt, eeq, tgt, teq;
-    block_scan2(gt, eq, egt, eeq, tgt, teq, warp_tot);
-    int pgt = base_gt + egt, peq = base_eq + eeq;
+    __syncthreads();
+    // exclusive sums over (item, warp), which is the order of the slots
+    int2 mine = make_int2(0, 0), inc;
+    if (threadIdx.x < kSelItems * 32) mine = counts[threadIdx.x];
+    inc = mine;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const bool valid = j0 + t < m, is_gt = valid && e[t] > thr, is_eq = valid && e[t] == thr;
-      if (is_gt || (is_eq && peq < need_eq)) kout[pgt + min(peq, need_eq)] = a.keep_first + j0 + t;
-      pgt += is_gt ? 1 : 0;
-      peq += is_eq ? 1 : 0;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, inc.x, o), y = __shfl_up_sync(0xffffffffu, inc.y, o);
+      if (lane >= o) { inc.x += x; inc.y += y; }
     }
-    base_gt += tgt;
-    base_eq += teq;
+    if (lane == 31) warp_tot2[warp] = inc;
+    __syncthreads();
+    const int2 t = warp_tot2[lane];
+    const int bx = __reduce_add_sync(0xffffffffu, lane < warp ? t.x : 0), by = __reduce_add_sync(0xffffffffu, lane < warp ? t.y : 0);
+    const int tx = __reduce_add_sync(0xffffffffu, t.x), ty = __reduce_add_sync(0xffffffffu, t.y);
+    if (threadIdx.x < kSelItems * 32) counts[threadIdx.x] = make_int2(bx + inc.x - mine.x, by + inc.y - mine.y);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSelItems; ++i) {
+      const int j = tile + i * kSelThreads + threadIdx.x;
+      const bool gt = j < m && key[i] > thr, eq = j < m && key[i] == thr;
+      const uint32_t lower = (1u << lane) - 1u;
+      const int pg = base_gt + counts[i * 32 + warp].x + __popc(__ballot_sync(0xffffffffu, gt) & lower);
+      const int pe = base_eq + counts[i * 32 + warp].y + __popc(__ballot_sync(0xffffffffu, eq) & lower);
+      if (gt || (eq && pe < need_eq)) kout[pg + min(pe, need_eq)] = a.keep_first + j;
+    }
+    base_gt += tx;
+    base_eq += ty;
+    __syncthreads();
   }
 }
 
@@ -322,16 +384,11 @@ __global__ void __launch_bounds__(kThreads) kv_gather_kernel(KvView c, EvictArgs
 #pragma unroll
   for (int i = 0; i < kMaxVec; ++i) {
     const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    uint32_t top = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y[4];
-      kv_decode4<FMT>(w[j], y);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t u = __float_as_uint(y[e] * s[i]) & 0x7FFFFFFFu;
-        big = max(big, u < 0x7F800000u ? u : 0u);
-      }
-    }
+    for (int j = 0; j < 4; ++j) top = kv_max_code<FMT>(w[j], top);
+    const uint32_t u = __float_as_uint(kv_max_value<FMT>(top) * s[i]);
+    big = max(big, u < 0x7F800000u ? u : 0u);
   }
   big = block_max(big, warp_max);
   const int page = a.dst_table ? kv_page(a.dst_table + b * a.dst_stride, column, a.dst_pages, c.status)
@@ -344,14 +401,17 @@ __global__ void __launch_bounds__(kThreads) kv_gather_kernel(KvView c, EvictArgs
   for (int i = 0; i < kMaxVec; ++i) {
     const int v = threadIdx.x + i * kThreads;
     if (v < nvec) {
+      if (s[i] == scale) {                                // the codes stay what they are
+        dst[v] = x[i];
+        continue;
+      }
       uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      const float f = s[i] * inv;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float y[4];
         kv_decode4<FMT>(w[j], y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = y[e] * s[i] * inv;
-        w[j] = kv_encode4<FMT>(y);
+        w[j] = kv_encode4_finite<FMT>(y, f);
       }
       dst[v] = make_uint4(w[0], w[1], w[2], w[3]);
     }

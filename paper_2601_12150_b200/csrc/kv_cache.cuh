@@ -104,6 +104,39 @@ template <int FMT>
 __device__ __forceinline__ uint32_t kv_encode4(const float* x) {
   return kv_code<FMT>(x[0]) | kv_code<FMT>(x[1]) << 8 | kv_code<FMT>(x[2]) << 16 | kv_code<FMT>(x[3]) << 24;
 }
+// The codes of x[i] * f where every one is known to be finite and at most the largest code.  int8: added to 1.5 * 2^23 a
+// number is rounded to an integer, to even, and its low byte is the code.
+template <int FMT>
+__device__ __forceinline__ uint32_t kv_encode4_finite(const float* x, float f) {
+  if (FMT == SPV_KV_INT8) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(fmaf(x[i], f, 12582912.0f));
+    return __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+  }
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(x[0] * f, x[1] * f), __NV_SATFINITE, __NV_E4M3);
+  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(x[2] * f, x[3] * f), __NV_SATFINITE, __NV_E4M3);
+  return lo | hi << 16;
+}
+// Largest magnitude of the codes in a word joined with `m`: two 16-bit lanes of magnitude bits.
+template <int FMT>
+__device__ __forceinline__ uint32_t kv_max_code(uint32_t w, uint32_t m) {
+  if (FMT == SPV_KV_INT8) {
+    uint32_t neg;                                          // 0xFF in the negative bytes: prmt's copies of a byte's sign
+    asm("prmt.b32 %0, %1, 0, 0xBA98;" : "=r"(neg) : "r"(w));
+    w = (w ^ neg) + (neg & 0x01010101u);
+  } else {
+    w &= 0x7F7F7F7Fu;
+  }
+  return __vmaxu2(m, __vmaxu2(w & 0x00FF00FFu, (w >> 8) & 0x00FF00FFu));
+}
+template <int FMT>
+__device__ __forceinline__ float kv_max_value(uint32_t m) {
+  m = max(m & 0xFFFFu, m >> 16);
+  float y[4];
+  kv_decode4<FMT>(m, y);
+  return fabsf(y[0]);
+}
 
 // two 16-bit values <-> fp32
 template <int DT>
