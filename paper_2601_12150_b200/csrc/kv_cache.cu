@@ -1,10 +1,10 @@
 // 8-bit key/value cache: append, eviction by accumulated attention weight, read-back.
 //
-//   kv_append_kernel   one CTA per touched (page, head, keys | values): the new rows stay in registers between
-//                      the largest-magnitude reduction and the conversion, so each crosses HBM once;
+//   kv_append_kernel   one CTA per touched (page, head): the new rows of keys and values stay in registers between the
+//                      largest-magnitude reduction and the conversion, so each crosses HBM once;
 //   kv_select_kernel   one CTA per (sequence, head): radix select of the survivors, ascending slots;
-//   kv_gather_kernel   one CTA per destination (page, head, keys | values): gathers the survivors' codes, which
-//                      stay in registers while the block's new scale is found;
+//   kv_gather_kernel   one CTA per destination (page, head): gathers the survivors' codes, which stay in registers
+//                      while the block's new scales are found;
 //   kv_place_kernel    eviction in place only: staged pages back over the sequence's own;
 //   kv_read_kernel     codes to 16- or 32-bit rows.
 #include "kv_cache.cuh"
@@ -18,14 +18,16 @@ using namespace spv;
 
 constexpr int kThreads = 256;
 
-// Largest of the threads' values, in every thread.
-__device__ __forceinline__ uint32_t block_max(uint32_t x, uint32_t* warp_max) {
-  x = __reduce_max_sync(0xffffffffu, x);
-  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = x;
+// Largest of the threads' values, of keys and of values, in every thread.  Called by all kThreads threads; `tmp` may be
+// written again after the next barrier.
+__device__ __forceinline__ uint2 block_max(uint2 x, uint2* tmp) {
+  x.x = __reduce_max_sync(0xffffffffu, x.x);
+  x.y = __reduce_max_sync(0xffffffffu, x.y);
+  if ((threadIdx.x & 31) == 0) tmp[threadIdx.x >> 5] = x;
   __syncthreads();
-  uint32_t m = warp_max[0];
+  uint2 m = tmp[0];
 #pragma unroll
-  for (int i = 1; i < kThreads / 32; ++i) m = max(m, warp_max[i]);
+  for (int i = 1; i < kThreads / 32; ++i) m = make_uint2(max(m.x, tmp[i].x), max(m.y, tmp[i].y));
   return m;
 }
 
@@ -33,105 +35,117 @@ struct AppendArgs {
   const uint16_t* src[2];
   int64_t stride_b, stride_tok, stride_head;
   const int32_t* counts;
-  int32_t tokens, block;
+  int32_t tokens;
 };
 
-template <int FMT, int DT, int D>
+// What a thread holds of a page: 16-byte vectors, all of the keys' before all of the values'.  Keys and values are
+// handled together: the chain of loads that leads to them (length, page, scale) is paid once, and twice as many are in
+// flight at its end.
+template <int FMT, int DT, int D, int BLOCK>
 __global__ void __launch_bounds__(kThreads) kv_append_kernel(KvView c, AppendArgs a) {
-  constexpr int kVecRow = D / 8;                          // 16-byte vectors of a new row
-  constexpr int kMaxVec = 128 * kVecRow / kThreads;       // of a whole block, per thread
-  __shared__ uint32_t warp_max[kThreads / 32];
-  const int b = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1;
+  constexpr int kVecRow = D / 8, kHalf = BLOCK * kVecRow;             // vectors of 8 new values
+  constexpr int kMine = (2 * kHalf + kThreads - 1) / kThreads;
+  __shared__ uint2 tmp[2][kThreads / 32];
+  const int b = blockIdx.z, head = blockIdx.y;
   const int len = kv_clamped(__ldg(c.lengths + b), c.max_length, c.status);
   int cnt = a.counts ? kv_clamped(__ldg(a.counts + b), a.tokens, c.status) : a.tokens;
   cnt = kv_clamped(cnt, c.max_length - len, c.status);
-  const SpvKvSpan span = spv_kv_append_span(len, cnt, a.block, blockIdx.x);
-  const int lo = span.lo, hi = span.hi;
-  if (lo >= hi) return;
+  const SpvKvSpan span = spv_kv_append_span(len, cnt, BLOCK, blockIdx.x);
+  const int lo = span.lo, rows = span.hi - lo;
+  if (rows <= 0) return;
   const int page = kv_page(c.table + b * c.table_stride, span.column, c.pages, c.status);
   if (page < 0) return;
-  const uint16_t* src = a.src[which] + b * a.stride_b + (int64_t)(lo - len) * a.stride_tok + head * a.stride_head;
-  const int nvec = (hi - lo) * kVecRow;
-  uint4 x[kMaxVec];
+  const int64_t from = b * a.stride_b + (int64_t)(lo - len) * a.stride_tok + head * a.stride_head;
+  uint4 x[kMine];
 #pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
-    const int v = threadIdx.x + i * kThreads;
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kThreads, which = v >= kHalf, r = v % kHalf / kVecRow;
     x[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (v < nvec) x[i] = __ldcs(reinterpret_cast<const uint4*>(src + (v / kVecRow) * a.stride_tok) + v % kVecRow);
-  }
-  uint32_t top = 0;                                       // magnitudes, two 16-bit lanes
-#pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) top = __vmaxu2(top, w[j] & 0x7FFF7FFFu);
+    if (v < 2 * kHalf && r < rows)
+      x[i] = __ldcs(reinterpret_cast<const uint4*>(a.src[which] + from + r * a.stride_tok) + v % kVecRow);
   }
   constexpr uint32_t kInf = DT == SPV_BF16 ? 0x7F80u : 0x7C00u;
-  uint32_t big = block_max(max(top & 0xFFFFu, top >> 16), warp_max);
-  const bool odd = big >= kInf;                           // infinities or NaN among them: the largest of the others
+  uint2 top = make_uint2(0u, 0u);                         // magnitudes, two 16-bit lanes
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const bool which = threadIdx.x + i * kThreads >= kHalf;
+    const uint32_t m = __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu),
+                                __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+    if (which) top.y = __vmaxu2(top.y, m);
+    else top.x = __vmaxu2(top.x, m);
+  }
+  uint2 big = block_max(make_uint2(max(top.x & 0xFFFFu, top.x >> 16), max(top.y & 0xFFFFu, top.y >> 16)), tmp[0]);
+  const bool odd = max(big.x, big.y) >= kInf;             // infinities or NaN among them: the largest of the others
   if (odd) {
     if (threadIdx.x == 0) kv_fault(c.status, SPV_SITE_KV_VALUE);
-    uint32_t fine = 0;
+    uint2 fine = make_uint2(0u, 0u);
 #pragma unroll
-    for (int i = 0; i < kMaxVec; ++i) {
+    for (int i = 0; i < kMine; ++i) {
+      const bool which = threadIdx.x + i * kThreads >= kHalf;
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint32_t p = w[j] & 0x7FFFu, q = w[j] >> 16 & 0x7FFFu;
-        fine = max(fine, max(p < kInf ? p : 0u, q < kInf ? q : 0u));
+        const uint32_t m = max(p < kInf ? p : 0u, q < kInf ? q : 0u);
+        if (which) fine.y = max(fine.y, m);
+        else fine.x = max(fine.x, m);
       }
     }
-    __syncthreads();                                      // warp_max is read no more
-    big = block_max(fine, warp_max);
+    big = block_max(fine, tmp[1]);
   }
-  big = __float_as_uint(kv_unpack2<DT>(big).x);
-  float* scale_at = const_cast<float*>(which ? c.v_scale : c.k_scale) + (size_t)page * c.kv_heads + head;
-  uint8_t* codes = const_cast<uint8_t*>(which ? c.v : c.k) + ((size_t)page * c.kv_heads + head) * a.block * D;
-  float scale = kv_pow2(kv_exponent<FMT>(big));
+  const size_t ph = (size_t)page * c.kv_heads + head;
   const int held = lo - span.base;                        // rows that were there before the call
-  if (held > 0) {
-    const float old = *scale_at;
-    if (!(scale > old)) {
-      scale = old;
-    } else {
-      const float f = old / scale;
-      for (int v = threadIdx.x; v < held * (D / 16); v += kThreads) {
-        uint4* at = reinterpret_cast<uint4*>(codes) + v;
-        const uint4 t = *at;
-        uint32_t w[4] = {t.x, t.y, t.z, t.w};
+  float scale[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float y[4];
-          kv_decode4<FMT>(w[j], y);
-          w[j] = kv_encode4_finite<FMT>(y, f);
+  for (int m = 0; m < 2; ++m) {
+    const uint32_t bits = __float_as_uint(kv_unpack2<DT>(m ? big.y : big.x).x);
+    scale[m] = kv_pow2(kv_exponent<FMT>(bits));
+    if (held > 0) {
+      const float old = (m ? c.v_scale : c.k_scale)[ph];
+      if (!(scale[m] > old)) {
+        scale[m] = old;
+      } else {
+        const float f = old / scale[m];
+        uint4* at = reinterpret_cast<uint4*>(const_cast<uint8_t*>(m ? c.v : c.k) + ph * BLOCK * D);
+        for (int v = threadIdx.x; v < held * (D / 16); v += kThreads) {
+          const uint4 t = at[v];
+          uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float y[4];
+            kv_decode4<FMT>(w[j], y);
+            w[j] = kv_encode4_finite<FMT>(y, f);
+          }
+          at[v] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        *at = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
-  const float inv = 1.0f / scale;
+  const float inv[2] = {1.0f / scale[0], 1.0f / scale[1]};
 #pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
-    const int v = threadIdx.x + i * kThreads;
-    if (v < nvec) {
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kThreads, which = v >= kHalf, r = v % kHalf / kVecRow;
+    if (v < 2 * kHalf && r < rows) {
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      const float f = which ? inv[1] : inv[0];
       uint32_t out[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const float2 p = kv_unpack2<DT>(w[2 * j]), q = kv_unpack2<DT>(w[2 * j + 1]);
         const float y[4] = {p.x, p.y, q.x, q.y};
         if (odd) {
-          const float z[4] = {y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+          const float z[4] = {y[0] * f, y[1] * f, y[2] * f, y[3] * f};
           out[j] = kv_encode4<FMT>(z);
         } else {
-          out[j] = kv_encode4_finite<FMT>(y, inv);
+          out[j] = kv_encode4_finite<FMT>(y, f);
         }
       }
-      *reinterpret_cast<uint2*>(codes + (size_t)(held + v / kVecRow) * D + (v % kVecRow) * 8) = make_uint2(out[0], out[1]);
+      uint8_t* codes = const_cast<uint8_t*>(which ? c.v : c.k) + (ph * BLOCK + held + r) * D;
+      *reinterpret_cast<uint2*>(codes + v % kVecRow * 8) = make_uint2(out[0], out[1]);
     }
   }
-  __syncthreads();                                        // every thread has read the old scale
-  if (threadIdx.x == 0) *scale_at = scale;
+  __syncthreads();                                        // every thread has read the old scales
+  if (threadIdx.x < 2) const_cast<float*>(threadIdx.x ? c.v_scale : c.k_scale)[ph] = threadIdx.x ? scale[1] : scale[0];
 }
 
 struct ReadArgs {
@@ -343,80 +357,82 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
   }
 }
 
-template <int FMT, int D>
+template <int FMT, int D, int BLOCK>
 __global__ void __launch_bounds__(kThreads) kv_gather_kernel(KvView c, EvictArgs a) {
-  constexpr int kVecRow = D / 16;
-  constexpr int kMaxVec = 128 * kVecRow / kThreads;
-  __shared__ uint32_t warp_max[kThreads / 32];
-  const int b = blockIdx.z, head = blockIdx.y >> 1, which = blockIdx.y & 1, column = blockIdx.x;
+  constexpr int kVecRow = D / 16, kHalf = BLOCK * kVecRow;            // vectors of 16 codes; keys, then values
+  constexpr int kMine = (2 * kHalf + kThreads - 1) / kThreads;
+  __shared__ uint2 tmp[kThreads / 32];
+  __shared__ int s_page[BLOCK], s_slot[BLOCK];            // of the survivors: page of the source, slot
+  const int b = blockIdx.z, head = blockIdx.y, column = blockIdx.x;
   const int len = min(max(__ldg(c.lengths + b), 0), c.max_length);
   const int n = min(len, a.budget);
-  const int base = column * a.block, rows = min(a.block, n - base);
+  const int base = column * BLOCK, rows = min(BLOCK, n - base);
   if (rows <= 0) return;
-  const int32_t* kept = a.kept + ((size_t)b * c.kv_heads + head) * a.budget + base;
-  const int32_t* row = c.table + b * c.table_stride;
-  const uint8_t* src = which ? c.v : c.k;
-  const float* src_scale = which ? c.v_scale : c.k_scale;
-  if (which == 0 && a.weights_out) {
-    const float* w = a.weights + b * a.w_stride_b + head * a.w_stride_head;
-    float* out = a.weights_out + ((size_t)b * c.kv_heads + head) * a.budget + base;
-    for (int t = threadIdx.x; t < rows; t += kThreads) out[t] = __ldg(w + kept[t]);
+  const size_t pair = (size_t)b * c.kv_heads + head;
+  if ((int)threadIdx.x < rows) {
+    const int slot = a.kept[pair * a.budget + base + threadIdx.x];
+    s_slot[threadIdx.x] = slot;
+    s_page[threadIdx.x] = kv_page(c.table + b * c.table_stride, slot / BLOCK, c.pages, c.status);
+    if (a.weights_out)
+      a.weights_out[pair * a.budget + base + threadIdx.x] = __ldg(a.weights + b * a.w_stride_b + head * a.w_stride_head + slot);
   }
-  const int nvec = rows * kVecRow;
-  uint4 x[kMaxVec];
-  float s[kMaxVec];
-  uint32_t big = 0;
+  const int page = a.dst_table ? kv_page(a.dst_table + b * a.dst_stride, column, a.dst_pages, c.status)
+                               : b * a.dst_blocks + column;
+  __syncthreads();
+  uint4 x[kMine];
+  float s[kMine];
+  uint2 big = make_uint2(0u, 0u);
 #pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
-    const int v = threadIdx.x + i * kThreads;
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kThreads, which = v >= kHalf, r = v % kHalf / kVecRow;
     x[i] = make_uint4(0u, 0u, 0u, 0u);
     s[i] = 0.0f;
-    if (v < nvec) {
-      const int slot = kept[v / kVecRow];
-      const int page = kv_page(row, slot / a.block, c.pages, c.status);
-      if (page >= 0) {
-        const size_t ph = (size_t)page * c.kv_heads + head;
-        x[i] = __ldcs(reinterpret_cast<const uint4*>(src + spv_kv_row(page, c.kv_heads, head, a.block, slot) * D) + v % kVecRow);
-        s[i] = __ldg(src_scale + ph);
+    if (v < 2 * kHalf && r < rows) {
+      const int from = s_page[r];
+      if (from >= 0) {
+        const int64_t row = spv_kv_row(from, c.kv_heads, head, BLOCK, s_slot[r]);
+        x[i] = __ldcs(reinterpret_cast<const uint4*>((which ? c.v : c.k) + row * D) + v % kVecRow);
+        s[i] = __ldg((which ? c.v_scale : c.k_scale) + (size_t)from * c.kv_heads + head);
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
+  for (int i = 0; i < kMine; ++i) {
     const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) top = kv_max_code<FMT>(w[j], top);
-    const uint32_t u = __float_as_uint(kv_max_value<FMT>(top) * s[i]);
-    big = max(big, u < 0x7F800000u ? u : 0u);
+    uint32_t u = __float_as_uint(kv_max_value<FMT>(top) * s[i]);
+    u = u < 0x7F800000u ? u : 0u;
+    if (threadIdx.x + i * kThreads >= kHalf) big.y = max(big.y, u);
+    else big.x = max(big.x, u);
   }
-  big = block_max(big, warp_max);
-  const int page = a.dst_table ? kv_page(a.dst_table + b * a.dst_stride, column, a.dst_pages, c.status)
-                               : b * a.dst_blocks + column;
+  big = block_max(big, tmp);
   if (page < 0) return;
-  const float scale = kv_pow2(kv_exponent<FMT>(big)), inv = 1.0f / scale;
+  const float scale[2] = {kv_pow2(kv_exponent<FMT>(big.x)), kv_pow2(kv_exponent<FMT>(big.y))};
+  const float inv[2] = {1.0f / scale[0], 1.0f / scale[1]};
   const size_t ph = (size_t)page * c.kv_heads + head;
-  uint4* dst = reinterpret_cast<uint4*>((which ? a.dst_v : a.dst_k) + ph * a.block * D);
 #pragma unroll
-  for (int i = 0; i < kMaxVec; ++i) {
-    const int v = threadIdx.x + i * kThreads;
-    if (v < nvec) {
-      if (s[i] == scale) {                                // the codes stay what they are
-        dst[v] = x[i];
+  for (int i = 0; i < kMine; ++i) {
+    const int v = threadIdx.x + i * kThreads, which = v >= kHalf, r = v % kHalf / kVecRow;
+    if (v < 2 * kHalf && r < rows) {
+      uint4* dst = reinterpret_cast<uint4*>((which ? a.dst_v : a.dst_k) + ph * BLOCK * D) + v % kHalf;
+      if (s[i] == (which ? scale[1] : scale[0])) {        // the codes stay what they are
+        *dst = x[i];
         continue;
       }
       uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-      const float f = s[i] * inv;
+      const float f = s[i] * (which ? inv[1] : inv[0]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float y[4];
         kv_decode4<FMT>(w[j], y);
         w[j] = kv_encode4_finite<FMT>(y, f);
       }
-      dst[v] = make_uint4(w[0], w[1], w[2], w[3]);
+      *dst = make_uint4(w[0], w[1], w[2], w[3]);
     }
   }
-  if (threadIdx.x == 0) (which ? a.dst_vs : a.dst_ks)[ph] = scale;
+  if (threadIdx.x < 2) (threadIdx.x ? a.dst_vs : a.dst_ks)[ph] = threadIdx.x ? scale[1] : scale[0];
 }
 
 // Staged page b * dst_blocks + column over page `column` of sequence b: the rows that hold survivors, and the scale.
@@ -445,6 +461,18 @@ void by_format(const spv_kv_cache* c, F f) {
     if (c->head_dim == 64) f(std::integral_constant<int, SPV_KV_E4M3>(), std::integral_constant<int, 64>());
     else f(std::integral_constant<int, SPV_KV_E4M3>(), std::integral_constant<int, 128>());
   }
+}
+
+template <typename F>
+void by_block(const spv_kv_cache* c, F f) {
+  by_format(c, [&](auto fmt, auto dim) {
+    switch (c->block) {
+      case 16: f(fmt, dim, std::integral_constant<int, 16>()); break;
+      case 32: f(fmt, dim, std::integral_constant<int, 32>()); break;
+      case 64: f(fmt, dim, std::integral_constant<int, 64>()); break;
+      default: f(fmt, dim, std::integral_constant<int, 128>()); break;
+    }
+  });
 }
 
 inline bool unaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
@@ -522,15 +550,14 @@ extern "C" int32_t kv_cache_append(spv_ctx* ctx, const spv_kv_cache* cache, cons
   a.stride_head = d->stride_head;
   a.counts = d->counts;
   a.tokens = d->tokens;
-  a.block = cache->block;
   // blocks that `tokens` new rows can touch, wherever in a block they begin
   const int64_t most = ((int64_t)d->tokens + cache->block - 2) / cache->block + 1;
   const unsigned nb = (unsigned)(most < seqs->columns ? most : seqs->columns);
-  const dim3 grid(nb, 2 * cache->kv_heads, seqs->batch);
+  const dim3 grid(nb, cache->kv_heads, seqs->batch);
   SpvProfScope prof(ctx, SPV_K_KV_CACHE, stream);
-  by_format(cache, [&](auto fmt, auto dim) {
-    if (d->dtype == SPV_BF16) kv_append_kernel<fmt(), SPV_BF16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
-    else kv_append_kernel<fmt(), SPV_FP16, dim()><<<grid, kThreads, 0, stream>>>(view, a);
+  by_block(cache, [&](auto fmt, auto dim, auto block) {
+    if (d->dtype == SPV_BF16) kv_append_kernel<fmt(), SPV_BF16, dim(), block()><<<grid, kThreads, 0, stream>>>(view, a);
+    else kv_append_kernel<fmt(), SPV_FP16, dim(), block()><<<grid, kThreads, 0, stream>>>(view, a);
   });
   return spv_launch_ok(ctx);
 }
@@ -624,8 +651,8 @@ extern "C" int32_t kv_cache_evict(spv_ctx* ctx, const spv_kv_cache* cache, const
   const dim3 grid(a.dst_blocks, 2 * cache->kv_heads, seqs->batch);
   SpvProfScope prof(ctx, SPV_K_KV_CACHE, stream);
   kv_select_kernel<<<dim3(cache->kv_heads, seqs->batch), kSelThreads, 0, stream>>>(view, a);
-  by_format(cache, [&](auto fmt, auto dim) {
-    kv_gather_kernel<fmt(), dim()><<<grid, kThreads, 0, stream>>>(view, a);
+  by_block(cache, [&](auto fmt, auto dim, auto block) {
+    kv_gather_kernel<fmt(), dim(), block()><<<dim3(a.dst_blocks, cache->kv_heads, seqs->batch), kThreads, 0, stream>>>(view, a);
   });
   if (!d->dst_table) {
     kv_place_kernel<<<grid, kThreads, 0, stream>>>(view, a, cache->head_dim / 16);
