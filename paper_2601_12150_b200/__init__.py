@@ -7,6 +7,7 @@ There is no CPU fallback.
 """
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libspatvit.so")
@@ -125,6 +126,16 @@ class KvReadDesc(C.Structure):
                 ("stride_head", C.c_int64), ("first", C.c_void_p)]
 
 
+# the same five as native layouts for struct.pack_into
+_KV_SEQS = struct.Struct("@iiqPPi4x")
+_KV_APPEND = struct.Struct("@iiqqqP")
+_KV_ATTN = struct.Struct("@iiiif4x8qP")
+_KV_EVICT = struct.Struct("@iii4xqqPq")
+_KV_READ = struct.Struct("@iiqqqP")
+assert [s.size for s in (_KV_SEQS, _KV_APPEND, _KV_ATTN, _KV_EVICT, _KV_READ)] == \
+    [C.sizeof(t) for t in (KvSeqs, KvAppendDesc, KvAttnDesc, KvEvictDesc, KvReadDesc)]
+
+
 MICROBENCH_KINDS = {"ex2": 0, "softmax_body": 1, "mma_ss": 2, "mma_ts": 3, "l2_tma": 4}
 
 
@@ -176,13 +187,14 @@ def lib():
                                     C.c_void_p]
         L.spv_layernorm.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
                                     C.c_float, C.c_void_p, C.c_void_p, C.c_void_p]
-        kv = [C.c_void_p, C.POINTER(KvCacheStruct), C.POINTER(KvSeqs)]
-        L.kv_cache_append.argtypes = kv + [C.POINTER(KvAppendDesc)] + [C.c_void_p] * 3
-        L.spv_kv_attention_workspace_size.argtypes = kv[1:] + [C.POINTER(KvAttnDesc), C.c_int32, C.POINTER(C.c_size_t)]
-        L.kv_cache_attention.argtypes = kv + [C.POINTER(KvAttnDesc)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
-        L.spv_kv_evict_workspace_size.argtypes = kv[1:] + [C.POINTER(KvEvictDesc), C.POINTER(C.c_size_t)]
-        L.kv_cache_evict.argtypes = kv + [C.POINTER(KvEvictDesc)] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
-        L.kv_cache_read.argtypes = kv + [C.POINTER(KvReadDesc)] + [C.c_void_p] * 3
+        # the cache calls' descriptors are passed by address (struct.pack_into is faster than building a Structure)
+        p = C.c_void_p
+        L.kv_cache_append.argtypes = [p] * 7
+        L.spv_kv_attention_workspace_size.argtypes = [p, p, p, C.c_int32, C.POINTER(C.c_size_t)]
+        L.kv_cache_attention.argtypes = [p] * 10 + [C.c_size_t, p]
+        L.spv_kv_evict_workspace_size.argtypes = [p, p, p, C.POINTER(C.c_size_t)]
+        L.kv_cache_evict.argtypes = [p] * 9 + [C.c_size_t, p]
+        L.kv_cache_read.argtypes = [p] * 7
         L.spv_profile_enable.argtypes = [C.c_void_p, C.c_int32]
         L.spv_profile_read.argtypes = [C.c_void_p, C.POINTER(KernelStat)]
         L.spv_selftest_wait.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p]
@@ -206,6 +218,13 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+def _raw_stream(device):
+    """The current stream of a device as an address, without making a torch.cuda.Stream of it where torch allows that."""
+    import torch
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device) if get else torch.cuda.current_stream(device).cuda_stream
+
+
 def _raise(status, what):
     if status != OK:
         raise SpvError(status, what)
@@ -217,10 +236,17 @@ def _need(ok, what):
         raise SpvError(ERR_INVALID_ARG, what)
 
 
-def _apart(t):
+def _apart(strides, shape):
     """Whether an output's strides are those of a view in which the elements do not overlap."""
+    reach = 1
+    for stride, n in zip(reversed(strides), reversed(shape)):      # the usual order: every dimension beyond those after it
+        if n > 1 and stride < reach:
+            break
+        reach = max(reach, stride * n)
+    else:
+        return True
     reach = 0
-    for stride, n in sorted(zip(t.stride(), t.shape)):
+    for stride, n in sorted(zip(strides, shape)):
         if n > 1:
             if stride <= reach:
                 return False
@@ -290,10 +316,11 @@ class KvCache:
                   "scales: contiguous fp32 [pages, kv_heads]")
         _need(k.is_cuda and all(t.device == k.device for t in (v, k_scale, v_scale)), "one CUDA device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device, self.device_index = k.device, k.get_device()
         self.pages, self.kv_heads, self.block, self.head_dim = k.shape
         self.struct = KvCacheStruct(self.pages, self.kv_heads, self.head_dim, self.block, fmt, k.data_ptr(),
                                     v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.address = C.addressof(self.struct)
 
     @classmethod
     def empty(cls, pages, kv_heads, head_dim, block=64, format=KV_INT8, device="cuda"):
@@ -318,6 +345,10 @@ class Context:
             _raise(lib().spv_create(C.byref(h), device), "spv_create")
         self.handle = h
         self._ws = None
+        self._index = device
+        self._kv_types = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}
+        self._seqs, self._desc, self._size = C.create_string_buffer(_KV_SEQS.size), C.create_string_buffer(128), C.c_size_t(0)
+        self._seqs_at, self._desc_at = C.addressof(self._seqs), C.addressof(self._desc)
 
     def close(self):
         if self.handle:
@@ -428,19 +459,24 @@ class Context:
         return out, sc
 
     # -- 8-bit key/value cache ------------------------------------------------------------------
+    # A decoder's step is a few microseconds of GPU work, so these methods keep the host's part short: every argument is
+    # checked, by the cheapest expression that tells, and descriptors are packed into buffers of the context.
     def _kv_seqs(self, cache, page_table, lengths, max_length=0):
-        torch = self._torch
-        _need(cache.device == self.device == page_table.device == lengths.device, "cache, tables: the context's device")
+        """Packs spv_kv_seqs; returns the batch."""
         B, cols = page_table.shape
-        _need(page_table.dtype == torch.int32 and page_table.stride(1) == 1 and (B == 1 or page_table.stride(0) >= cols),
-              "page_table: int32 [batch, columns], rows apart")
-        _need(lengths.dtype == torch.int32 and lengths.shape == (B,) and lengths.is_contiguous(), "lengths: int32 [batch]")
-        return KvSeqs(B, cols, page_table.stride(0) if B > 1 else 0, page_table.data_ptr(), lengths.data_ptr(), max_length)
+        rows, inner = page_table.stride()
+        i32, dev = self._torch.int32, self._index
+        _need(cache.device_index == dev and page_table.get_device() == dev and page_table.dtype is i32 and inner == 1 and
+              (rows >= cols or B == 1), "page_table: int32 [batch, columns], rows apart, on the context's device, as the cache")
+        _need(lengths.dtype is i32 and lengths.shape == (B,) and lengths.is_contiguous() and lengths.get_device() == dev,
+              "lengths: int32 [batch]")
+        _KV_SEQS.pack_into(self._seqs, 0, B, cols, rows if B > 1 else 0, page_table.data_ptr(), lengths.data_ptr(), max_length)
+        return B
 
     def _kv_vector(self, t, B, what):
         if t is None:
-            return None
-        _need(t.dtype == self._torch.int32 and t.shape == (B,) and t.is_contiguous() and t.device == self.device,
+            return 0
+        _need(t.dtype is self._torch.int32 and t.shape == (B,) and t.is_contiguous() and t.get_device() == self._index,
               what + ": int32 [batch]")
         return t.data_ptr()
 
@@ -454,31 +490,35 @@ class Context:
         with self._torch.cuda.stream(stream):
             return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
 
+    def _kv_stream(self, stream):
+        if stream is not None:
+            return stream.cuda_stream
+        return _raw_stream(self._index)
+
     def _kv_dtype(self, t):
-        torch = self._torch
-        dt = {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(t.dtype)
-        _need(dt is not None and t.dim() == 4 and t.stride(3) == 1 and t.device == self.device,
+        dt = self._kv_types.get(t.dtype)
+        _need(dt is not None and t.dim() == 4 and t.stride(3) == 1 and t.get_device() == self._index,
               "bf16, fp16 (or, of kv_cache_read, fp32) [batch, tokens, heads, head_dim], head_dim contiguous, on the "
               "context's device")
         return dt
 
     def _kv_weights(self, cache, w, B):
-        _need(w.dtype == self._torch.float32 and w.dim() == 3 and w.shape[:2] == (B, cache.kv_heads) and
-              w.stride(2) == 1 and w.device == self.device, "weights: fp32 [batch, kv_heads, slots], slots contiguous")
+        _need(w.dtype is self._torch.float32 and w.dim() == 3 and w.shape[:2] == (B, cache.kv_heads) and
+              w.stride(2) == 1 and w.get_device() == self._index, "weights: fp32 [batch, kv_heads, slots], slots contiguous")
 
     def kv_cache_append(self, cache, k, v, page_table, lengths, counts=None, stream=None):
         """Quantise new tokens' keys and values into the cache, behind the `lengths` that each sequence holds.
         k, v: bf16 or fp16 [B, tokens, kv_heads, head_dim] views with the same strides; counts: int32 [B], new
         tokens of each sequence (default: all).  `lengths` is not changed: add the counts to it afterwards."""
         dt = self._kv_dtype(k)
-        B, n, h, d = k.shape
-        _need(v.dtype == k.dtype and v.shape == k.shape and v.stride() == k.stride() and v.device == k.device, "v: as k")
-        _need(h == cache.kv_heads and d == cache.head_dim and page_table.shape[0] == B, "k: the cache's heads and head_dim")
-        seqs = self._kv_seqs(cache, page_table, lengths)
-        sb, st, sh, _ = k.stride()
-        desc = KvAppendDesc(n, dt, sb, st, sh, self._kv_vector(counts, B, "counts"))
-        _raise(lib().kv_cache_append(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(k), _ptr(v),
-                                     _stream(stream)), "kv_cache_append")
+        shape, strides = k.shape, k.stride()
+        B, n, h, d = shape
+        _need(v.dtype is k.dtype and v.shape == shape and v.stride() == strides and v.get_device() == self._index, "v: as k")
+        _need(h == cache.kv_heads and d == cache.head_dim and self._kv_seqs(cache, page_table, lengths) == B,
+              "k: the cache's heads and head_dim, the table's batch")
+        _KV_APPEND.pack_into(self._desc, 0, n, dt, *strides[:3], self._kv_vector(counts, B, "counts"))
+        _raise(lib().kv_cache_append(self.handle, cache.address, self._seqs_at, self._desc_at, k.data_ptr(), v.data_ptr(),
+                                     self._kv_stream(stream)), "kv_cache_append")
 
     def kv_cache_attention(self, cache, q, page_table, lengths, counts=None, causal=True, scale=0.0, out=None, lse=None,
                            weights_in=None, weights_out=None, max_length=None, workspace=None, stream=None):
@@ -486,43 +526,49 @@ class Context:
         queries' own tokens.  counts: int32 [B], queries of each sequence (default: all; rows behind them are not
         written).  lse: optional fp32 [B, tokens, heads] to fill.  weights_out: optional fp32 [B, kv_heads, slots]:
         weights_in (default 0; may be weights_out itself) plus the attention weight that every kept token received.
-        max_length: no sequence is longer (default: what the table and the weights have room for).  Returns out."""
+        max_length: no sequence is longer (default: what the table and the weights have room for; the workspace grows
+        with it).  Returns out."""
         torch = self._torch
         dt = self._kv_dtype(q)
-        B, n, H, d = q.shape
-        _need(d == cache.head_dim and page_table.shape[0] == B, "q: [batch, tokens, heads, the cache's head_dim]")
+        shape = q.shape
+        B, n, H, d = shape
         if out is None:
-            out = torch.empty((B, n, H, d), dtype=q.dtype, device=q.device)
-        _need(out.dtype == q.dtype and out.shape == q.shape and out.stride(3) == 1 and out.device == q.device and
-              _apart(out), "out: as q, no two elements at one place")
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        o_strides = out.stride()
+        _need(out.dtype is q.dtype and out.shape == shape and o_strides[3] == 1 and out.get_device() == self._index and
+              _apart(o_strides, shape), "out: as q, no two elements at one place")
         limit = page_table.shape[1] * cache.block
-        wb = wh = 0
+        wb = wh = w_in_at = w_out_at = lse_at = 0
         if weights_out is not None:
             self._kv_weights(cache, weights_out, B)
-            _need(_apart(weights_out), "weights_out: no two elements at one place")
-            limit = min(limit, weights_out.shape[2])
             wb, wh, _ = weights_out.stride()
-            if weights_in is not None and weights_in is not weights_out:
+            limit = min(limit, weights_out.shape[2])
+            _need(_apart((wb, wh, 1), weights_out.shape), "weights_out: no two elements at one place")
+            w_out_at = weights_out.data_ptr()
+        if weights_in is not None:
+            _need(weights_out is not None, "weights_in: only with weights_out")
+            if weights_in is not weights_out:
                 self._kv_weights(cache, weights_in, B)
-                _need(weights_in.shape == weights_out.shape and weights_in.stride() == weights_out.stride(),
-                      "weights_in: as weights_out")
+                _need(weights_in.shape == weights_out.shape and weights_in.stride() == (wb, wh, 1), "weights_in: as weights_out")
+            w_in_at = weights_in.data_ptr()
         if max_length is not None:
             _need(1 <= max_length <= limit, "max_length: 1 .. what the table and the weights have room for")
             limit = max_length
         if lse is not None:
-            _need(lse.dtype == torch.float32 and lse.shape == (B, n, H) and lse.is_contiguous() and lse.device == q.device,
-                  "lse: fp32 [batch, tokens, heads]")
-        seqs = self._kv_seqs(cache, page_table, lengths, limit)
-        desc = KvAttnDesc(n, H, dt, int(causal), float(scale), *q.stride()[:3], *out.stride()[:3], wb, wh,
-                          self._kv_vector(counts, B, "counts"))
-        need = C.c_size_t(0)
-        _raise(lib().spv_kv_attention_workspace_size(C.byref(cache.struct), C.byref(seqs), C.byref(desc),
-                                                     weights_out is not None, C.byref(need)),
+            _need(lse.dtype is torch.float32 and lse.shape == (B, n, H) and lse.is_contiguous() and
+                  lse.get_device() == self._index, "lse: fp32 [batch, tokens, heads]")
+            lse_at = lse.data_ptr()
+        _need(d == cache.head_dim and self._kv_seqs(cache, page_table, lengths, limit) == B,
+              "q: [batch, tokens, heads, the cache's head_dim], the table's batch")
+        _KV_ATTN.pack_into(self._desc, 0, n, H, dt, 1 if causal else 0, scale, *q.stride()[:3], *o_strides[:3], wb, wh,
+                           self._kv_vector(counts, B, "counts"))
+        L, need = lib(), self._size
+        _raise(L.spv_kv_attention_workspace_size(cache.address, self._seqs_at, self._desc_at, 1 if w_out_at else 0, need),
                "spv_kv_attention_workspace_size")
         ws = self._kv_scratch(need.value, workspace, stream)
-        _raise(lib().kv_cache_attention(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(q),
-                                        _ptr(out), _ptr(lse), _ptr(weights_in), _ptr(weights_out), _ptr(ws),
-                                        0 if ws is None else ws.numel(), _stream(stream)), "kv_cache_attention")
+        _raise(L.kv_cache_attention(self.handle, cache.address, self._seqs_at, self._desc_at, q.data_ptr(), out.data_ptr(),
+                                    lse_at, w_in_at, w_out_at, 0 if ws is None else ws.data_ptr(),
+                                    0 if ws is None else ws.numel(), self._kv_stream(stream)), "kv_cache_attention")
         return out
 
     def kv_cache_evict(self, cache, weights, page_table, lengths, budget, keep_first=0, keep_last=0, dst_table=None,
@@ -533,39 +579,44 @@ class Context:
         sequence's own.  Returns (kept int32 [B, kv_heads, budget], new_lengths int32 [B], weights_out fp32
         [B, kv_heads, budget])."""
         torch = self._torch
-        self._kv_weights(cache, weights, page_table.shape[0])
         B, h = page_table.shape[0], cache.kv_heads
+        self._kv_weights(cache, weights, B)
         limit = min(page_table.shape[1] * cache.block, weights.shape[2])
         if max_length is not None:
             _need(1 <= max_length <= limit, "max_length: 1 .. what the table and the weights have room for")
             limit = max_length
-        seqs = self._kv_seqs(cache, page_table, lengths, limit)
-        _need(int(budget) >= 1, "budget: 1 or more")
+        self._kv_seqs(cache, page_table, lengths, limit)
+        _need(budget >= 1, "budget: 1 or more")
+        shape, dev = (B, h, budget), self._index
         if kept is None:
-            kept = torch.empty((B, h, budget), dtype=torch.int32, device=self.device)
+            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
         if weights_out is None:
-            weights_out = torch.zeros((B, h, budget), dtype=torch.float32, device=self.device)
+            weights_out = torch.zeros(shape, dtype=torch.float32, device=self.device)
         if new_lengths is None:
             new_lengths = torch.empty((B,), dtype=torch.int32, device=self.device)
-        _need(kept.dtype == torch.int32 and kept.shape == (B, h, budget) and kept.is_contiguous() and
-              kept.device == self.device, "kept: int32 [batch, kv_heads, budget]")
-        _need(weights_out.dtype == torch.float32 and weights_out.shape == kept.shape and weights_out.is_contiguous() and
-              weights_out.device == self.device, "weights_out: fp32 [batch, kv_heads, budget]")
+        _need(kept.dtype is torch.int32 and kept.shape == shape and kept.is_contiguous() and kept.get_device() == dev,
+              "kept: int32 [batch, kv_heads, budget]")
+        _need(weights_out.dtype is torch.float32 and weights_out.shape == shape and weights_out.is_contiguous() and
+              weights_out.get_device() == dev, "weights_out: fp32 [batch, kv_heads, budget]")
         nl = self._kv_vector(new_lengths, B, "new_lengths")
-        dst, stride = None, 0
+        dst = stride = 0
         if dst_table is not None:
-            _need(dst_table.dtype == torch.int32 and dst_table.dim() == 2 and dst_table.shape[0] == B and
-                  dst_table.stride(1) == 1 and dst_table.shape[1] * cache.block >= budget and
-                  (B == 1 or dst_table.stride(0) >= dst_table.shape[1]) and dst_table.device == self.device, "dst_table: int32 [batch, budget / block or more]")
-            dst, stride = dst_table.data_ptr(), dst_table.stride(0) if B > 1 else 0
-        desc = KvEvictDesc(budget, keep_first, keep_last, weights.stride(0), weights.stride(1), dst, stride)
-        need = C.c_size_t(0)
-        _raise(lib().spv_kv_evict_workspace_size(C.byref(cache.struct), C.byref(seqs), C.byref(desc), C.byref(need)),
-               "spv_kv_evict_workspace_size")
-        ws = self._kv_scratch(need.value, workspace, stream)
-        _raise(lib().kv_cache_evict(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(weights),
-                                    _ptr(kept), _ptr(weights_out), nl, _ptr(ws), 0 if ws is None else ws.numel(),
-                                    _stream(stream)), "kv_cache_evict")
+            rows, cols = dst_table.stride(0), dst_table.shape[1]
+            _need(dst_table.dtype is torch.int32 and dst_table.dim() == 2 and dst_table.shape[0] == B and
+                  dst_table.stride(1) == 1 and cols * cache.block >= budget and (B == 1 or rows >= cols) and
+                  dst_table.get_device() == dev, "dst_table: int32 [batch, budget / block or more], rows apart")
+            dst, stride = dst_table.data_ptr(), rows if B > 1 else 0
+        _KV_EVICT.pack_into(self._desc, 0, budget, keep_first, keep_last, weights.stride(0), weights.stride(1), dst, stride)
+        L, nbytes = lib(), 0
+        if dst_table is None:
+            need = self._size
+            _raise(L.spv_kv_evict_workspace_size(cache.address, self._seqs_at, self._desc_at, need),
+                   "spv_kv_evict_workspace_size")
+            nbytes = need.value
+        ws = self._kv_scratch(nbytes, workspace, stream)
+        _raise(L.kv_cache_evict(self.handle, cache.address, self._seqs_at, self._desc_at, weights.data_ptr(), kept.data_ptr(),
+                                weights_out.data_ptr(), nl, 0 if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(),
+                                self._kv_stream(stream)), "kv_cache_evict")
         return kept, new_lengths, weights_out
 
     def kv_cache_read(self, cache, page_table, counts, first=None, k_out=None, v_out=None, rows=None, dtype=None,
@@ -574,24 +625,25 @@ class Context:
         [B, rows, kv_heads, head_dim] (bf16, fp16 or fp32 views with the same strides; rows behind counts[b] are left
         as they were).  Without outputs, zeroed ones of `rows` rows and `dtype` (default bf16) are made; a single
         output may be given for only that half.  Returns (k_out, v_out)."""
-        torch = self._torch
-        B = page_table.shape[0]
         if k_out is None and v_out is None:
+            torch = self._torch
             rows = page_table.shape[1] * cache.block if rows is None else rows
-            shape = (B, rows, cache.kv_heads, cache.head_dim)
-            k_out = torch.zeros(shape, dtype=dtype or torch.bfloat16, device=self.device)
+            k_out = torch.zeros((page_table.shape[0], rows, cache.kv_heads, cache.head_dim), dtype=dtype or torch.bfloat16,
+                                device=self.device)
             v_out = torch.zeros_like(k_out)
         o = k_out if k_out is not None else v_out
         dt = self._kv_dtype(o)
-        _need(_apart(o) and o.shape[0] == B and o.shape[2:] == (cache.kv_heads, cache.head_dim), "outputs: [batch, rows, kv_heads, head_dim]")
+        shape, strides = o.shape, o.stride()
+        B = self._kv_seqs(cache, page_table, counts)
+        _need(shape[0] == B and shape[2] == cache.kv_heads and shape[3] == cache.head_dim and _apart(strides, shape),
+              "outputs: [batch, rows, kv_heads, head_dim], no two elements at one place")
         if k_out is not None and v_out is not None:
-            _need(v_out.dtype == o.dtype and v_out.shape == o.shape and v_out.stride() == o.stride() and
-                  v_out.device == o.device, "v_out: as k_out")
-        seqs = self._kv_seqs(cache, page_table, counts)
-        sb, st, sh, _ = o.stride()
-        desc = KvReadDesc(o.shape[1], dt, sb, st, sh, self._kv_vector(first, B, "first"))
-        _raise(lib().kv_cache_read(self.handle, C.byref(cache.struct), C.byref(seqs), C.byref(desc), _ptr(k_out),
-                                   _ptr(v_out), _stream(stream)), "kv_cache_read")
+            _need(v_out.dtype is o.dtype and v_out.shape == shape and v_out.stride() == strides and
+                  v_out.get_device() == self._index, "v_out: as k_out")
+        _KV_READ.pack_into(self._desc, 0, shape[1], dt, *strides[:3], self._kv_vector(first, B, "first"))
+        _raise(lib().kv_cache_read(self.handle, cache.address, self._seqs_at, self._desc_at,
+                                   0 if k_out is None else k_out.data_ptr(), 0 if v_out is None else v_out.data_ptr(),
+                                   self._kv_stream(stream)), "kv_cache_read")
         return k_out, v_out
 
     # -- building blocks ----------------------------------------------------------------------
