@@ -38,12 +38,12 @@ struct alignas(16) Stretch {
 
 struct StreamArgs {
   KvAttnArgs a;
-  float* z;             // scores (log2 domain) [tile][rows][slot], NULL when no weights are wanted
+  float* z;             // scores (log2 domain) [tile][pair of rows][slot][2], NULL when no weights are wanted
   float* part_o;        // [worker][2][8 NT][D] unnormalised
   float2* part_ml;      // [8 NT][2][worker] maximum, sum: a row's pieces side by side
   float2* pair_ml;      // [pair][8 NT]: the same of pairs that one worker had whole
   Stretch* stretch;     // [worker]
-  int32_t rows;         // tokens * group
+  int32_t rows;         // tokens * group, made even
 };
 
 struct StageMeta {      // of one tile, by 16-slot quarters
@@ -295,7 +295,9 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
   uint64_t policy;
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
   const int part = min(s.a.block, kTile);              // slots that one copy brings
-  const int parts = kTile / part;                      // copies of a tile: 1, 2 or 4
+  const int lparts = 31 - __clz(kTile / part);         // a tile has 2^lparts copies: 1, 2 or 4
+  const int parts = 1 << lparts;
+  const int lblock = 31 - __clz(s.a.block);
   const int stretch = walk.end - walk.pos;
   Walk fwalk = walk;
   Piece fp;
@@ -311,16 +313,16 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
       f_end += fp.kt1 - fp.kt0;
       f_batch = -1;
     }
-    int at = f_batch < 0 ? 32 : (it - f_batch) * parts;
+    int at = f_batch < 0 ? 32 : (it - f_batch) << lparts;
     if (at >= 32) {
       f_batch = it;
       at = 0;
-      const int mine = it + lane / parts, slot = (fp.kt0 + mine - f_begin) * kTile + lane % parts * part;
+      const int mine = it + (lane >> lparts), slot = (fp.kt0 + mine - f_begin) * kTile + (lane & (parts - 1)) * part;
       f_row = -1;
       f_lost = 0;
       f_ks = f_vs = 0.0f;                              // of parts that hold nothing
       if (mine < f_end && slot < fp.len) {
-        const int page = kv_page(c.table + fp.b * c.table_stride, slot / s.a.block, c.pages, c.status);
+        const int page = kv_page(c.table + fp.b * c.table_stride, slot >> lblock, c.pages, c.status);
         if (page >= 0) {
           const size_t ph = (size_t)page * c.kv_heads + fp.head;
           f_ks = __ldg(c.k_scale + ph);
@@ -331,27 +333,32 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
         }
       }
     }
-    const bool mine = lane >= at && lane < at + parts;
+    const int x0 = lane - at;                            // which copy of the tile is this lane's, if one is
+    const bool mine = x0 >= 0 && x0 < parts;
     const int loads = __popc(__ballot_sync(0xffffffffu, mine && f_row >= 0));
-    const uint32_t lost = __ballot_sync(0xffffffffu, mine && f_lost) >> at;
-    if (lane == at) {
+    const uint32_t lost = __ballot_sync(0xffffffffu, mine && f_lost);
+    if (x0 == 0) {
       mbar_expect_tx(full + st, loads * 2 * part * D);
       int bad = 0;
+      if (lost) {
 #pragma unroll
-      for (int x = 0; x < kQuarters; ++x) bad |= (int)(lost >> (x * parts / kQuarters) & 1u) << x;
+        for (int x = 0; x < kQuarters; ++x) bad |= (int)(lost >> (at + (x * parts / kQuarters)) & 1u) << x;
+      }
       meta[st].bad = bad;
     }
     __syncwarp();
     if (mine) {
-      const int x0 = lane - at;
       if (f_row >= 0) {
         uint8_t* dst = smem + st * L::kStageBytes + x0 * part * D;
         tma_load_rows(dst, &map_k, full + st, f_row, policy);
         tma_load_rows(dst + kTile * D, &map_v, full + st, f_row, policy);
       }
-      for (int x = x0 * kQuarters / parts; x < (x0 + 1) * kQuarters / parts; ++x) {
-        meta[st].ks[x] = f_ks;
-        meta[st].vs[x] = f_vs;
+#pragma unroll
+      for (int x = 0; x < kQuarters; ++x) {
+        if (x * parts / kQuarters == x0) {               // quarter x is in this copy
+          meta[st].ks[x] = f_ks;
+          meta[st].vs[x] = f_vs;
+        }
       }
     }
     __syncwarp();
@@ -477,21 +484,18 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
           }
         }
         if (s.z) {
-          float* zt = s.z + (size_t)(p.line + kt) * s.rows * kTile;
+          float2* zt = reinterpret_cast<float2*>(s.z + (size_t)(p.line + kt) * s.rows * kTile) + half * kKeys + r;
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
+          for (int t = 0; t < NT; ++t) {
+            if (8 * t + q2 < s.rows) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int row = 8 * t + q2 + e;
-              if (row < s.rows) {
-#pragma unroll
-                for (int i = 0; i < kMt; ++i) {
-                  float* at = zt + row * kTile + half * kKeys + i * 16 + r;
-                  at[0] = z[i][t][e];
-                  at[8] = z[i][t][e + 2];
-                }
+              for (int i = 0; i < kMt; ++i) {
+                float2* at = zt + (4 * t + (q2 >> 1)) * kTile + i * 16;
+                at[0] = make_float2(z[i][t][0], z[i][t][1]);
+                at[8] = make_float2(z[i][t][2], z[i][t][3]);
               }
             }
+          }
         }
         // running maxima: renewed for all when any score is far above its own
         float top[NT][2];
@@ -704,7 +708,7 @@ template <int D>
 __global__ void __launch_bounds__(kFinishThreads, 4)
     kv_finish_kernel(const KvView c, const StreamArgs s, int workers, int row_slots) {
   constexpr int kTile = tile_of(D);
-  __shared__ float2 stat[kKvStreamMaxRows];     // maximum, 1 / sum of a row
+  __shared__ float2 stat[kKvStreamMaxRows + 1]; // maximum, 1 / sum of a row
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int b = blockIdx.x; b < s.a.batch; b += gridDim.x)
     if (seq_key_tiles<kTile>(c, s.a, b) == 0) write_empty<D>(c, s.a, b);
@@ -727,6 +731,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     const int rows = p.n * s.a.group;
     const size_t pair = (size_t)(p.b * c.kv_heads + p.head) * row_slots;
     __syncthreads();                            // stat of the piece before is read no more
+    if ((rows & 1) && threadIdx.x == 0) stat[rows] = make_float2(0.0f, 0.0f);       // of the pair's row that there is not
     for (int row = warp; row < rows; row += kFinishThreads / 32) {
       const float2 ml = c0 == c1 ? s.pair_ml[pair + row] : joined(s, workers, c0, c1, row);
       if (lane == 0) {
@@ -788,7 +793,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     const bool wide = (((uintptr_t)w_out | (uintptr_t)w_in) & 15u) == 0;
     // four keys a thread: the scores of a row are side by side
     for (int key = p.kt0 * kTile + ((int)threadIdx.x - joiners) * 4; key < key1; key += joiners * 4) {
-      const float* zt = s.z + (size_t)(p.line + key / kTile) * s.rows * kTile + key % kTile;
+      const float* zt = s.z + (size_t)(p.line + key / kTile) * s.rows * kTile + key % kTile * 2;
       const bool four = wide && key + 4 <= key1;
       float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       if (w_in) {
@@ -802,14 +807,14 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
         }
       }
       float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-      for (int row = 0; row < rows; ++row) {
-        const float4 z = *reinterpret_cast<const float4*>(zt + row * kTile);
-        const float2 st = stat[row];
-        sum.x = fmaf(exp2_fast(z.x - st.x), st.y, sum.x);
-        sum.y = fmaf(exp2_fast(z.y - st.x), st.y, sum.y);
-        sum.z = fmaf(exp2_fast(z.z - st.x), st.y, sum.z);
-        sum.w = fmaf(exp2_fast(z.w - st.x), st.y, sum.w);
+#pragma unroll 2
+      for (int row = 0; row < rows; row += 2) {
+        const float4 u = *reinterpret_cast<const float4*>(zt + row * kTile), v = *reinterpret_cast<const float4*>(zt + row * kTile + 4);
+        const float2 s0 = stat[row], s1 = stat[row + 1];
+        sum.x = fmaf(exp2_fast(u.x - s0.x), s0.y, fmaf(exp2_fast(u.y - s1.x), s1.y, sum.x));
+        sum.y = fmaf(exp2_fast(u.z - s0.x), s0.y, fmaf(exp2_fast(u.w - s1.x), s1.y, sum.y));
+        sum.z = fmaf(exp2_fast(v.x - s0.x), s0.y, fmaf(exp2_fast(v.y - s1.x), s1.y, sum.z));
+        sum.w = fmaf(exp2_fast(v.z - s0.x), s0.y, fmaf(exp2_fast(v.w - s1.x), s1.y, sum.w));
       }
       w = make_float4(w.x + sum.x, w.y + sum.y, w.z + sum.z, w.w + sum.w);
       if (four) {
@@ -832,7 +837,7 @@ int row_slots_of(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32); }
 
 struct Workspace { size_t part_o, part_ml, pair_ml, stretch, z, total; };
 Workspace plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d, bool weights) {
-  const int rows = d->tokens * (d->heads / c->kv_heads), slots = row_slots_of(rows), tile = tile_of(c->head_dim);
+  const int rows = (d->tokens * (d->heads / c->kv_heads) + 1) & ~1, slots = row_slots_of(rows), tile = tile_of(c->head_dim);
   const size_t tiles = (size_t)q->batch * c->kv_heads * ((spv_kv_max_length(c, q) + tile - 1) / tile);
   Workspace w;
   const size_t workers = (size_t)kMaxSms * warps_of(slots);
@@ -875,7 +880,7 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   const KvView view = kv_view(ctx, cache, seqs);
   StreamArgs s;
   s.a = a;
-  s.rows = a.tokens * a.group;
+  s.rows = (a.tokens * a.group + 1) & ~1;
   char* base = (char*)workspace;
   s.part_o = (float*)(base + w.part_o);
   s.part_ml = (float2*)(base + w.part_ml);
