@@ -657,7 +657,6 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
 
 // ---- pieces and weights --------------------------------------------------------------------------
 constexpr int kFinishThreads = 256;
-__host__ __device__ constexpr int finish_workers(int row_slots) { return warps_of(row_slots) / 4; }   // of a block: four blocks an SM
 
 __device__ __forceinline__ const float2* part_ml(const StreamArgs& s, int workers, int row, int worker, int c0) {
   return s.part_ml + (size_t)(2 * row + (worker == c0)) * workers + worker;
@@ -706,19 +705,19 @@ __device__ __forceinline__ void write_empty(const KvView& c, const KvAttnArgs& a
 // A block takes the stretches of a few workers; half of its threads joins pieces while the other makes weights.
 template <int D>
 __global__ void __launch_bounds__(kFinishThreads, 4)
-    kv_finish_kernel(const KvView c, const StreamArgs s, int workers, int row_slots) {
+    kv_finish_kernel(const KvView c, const StreamArgs s, int workers, int row_slots, int per_block) {
   constexpr int kTile = tile_of(D);
   __shared__ float2 stat[kKvStreamMaxRows + 1]; // maximum, 1 / sum of a row
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int b = blockIdx.x; b < s.a.batch; b += gridDim.x)
     if (seq_key_tiles<kTile>(c, s.a, b) == 0) write_empty<D>(c, s.a, b);
-  const int first = blockIdx.x * finish_workers(row_slots);
+  const int first = blockIdx.x * per_block;
   const Stretch at = s.stretch[first];
   const Share share(at.total, workers);
   if (first >= share.working) return;
   Walk w;
   w.pos = share.begin(first);
-  w.end = share.begin(min(first + finish_workers(row_slots), share.working));
+  w.end = share.begin(min(first + per_block, share.working));
   w.before = at.before;
   w.b = at.b;
   Piece p{at.b, at.head, at.len, at.n, at.tiles, at.kt0, min(at.tiles, at.kt0 + w.end - w.pos), w.pos - at.kt0};
@@ -748,7 +747,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
       if (c0 == c1) continue;
       // the blocks that meet the pair share its columns (four values of a row), and as many threads as there are share
       // a column's pieces
-      const int f0 = c0 / finish_workers(row_slots), f1 = c1 / finish_workers(row_slots), mine = blockIdx.x - f0;
+      const int f0 = c0 / per_block, f1 = c1 / per_block, mine = blockIdx.x - f0;
       const int columns = rows * (D / 4);
       const int x0 = columns * mine / (f1 - f0 + 1), x1 = columns * (mine + 1) / (f1 - f0 + 1);
       const int lanes = x1 - x0 >= joiners ? 1 : min(32, 1 << (31 - __clz(joiners / max(1, x1 - x0))));
@@ -917,8 +916,11 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if (st != SPV_OK) return st;
   const int workers = ctas * warps_of(slots);
   const int64_t used = most < workers ? most : workers;
-  const unsigned blocks = (unsigned)((used + finish_workers(slots) - 1) / finish_workers(slots));
-  if (cache->head_dim == 64) kv_finish_kernel<64><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots);
-  else kv_finish_kernel<128><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots);
+  // as many blocks as are resident at once, four an SM; of few workers each has its own (785 slots, 16 heads: 12.7 us for
+  // the step instead of 15 with three to a block)
+  const int per_block = (int)((used + 4 * ctas - 1) / (4 * ctas));
+  const unsigned blocks = (unsigned)((used + per_block - 1) / per_block);
+  if (cache->head_dim == 64) kv_finish_kernel<64><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots, per_block);
+  else kv_finish_kernel<128><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots, per_block);
   return spv_launch_ok(ctx, 2);
 }
