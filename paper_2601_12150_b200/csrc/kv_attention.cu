@@ -15,8 +15,8 @@ int32_t check_attn(const spv_kv_cache* c, const spv_kv_seqs* s, const spv_kv_att
   if (!(d->softmax_scale >= 0.0f) || d->softmax_scale > 1e30f) return SPV_ERR_INVALID_ARG;
   if ((int64_t)d->tokens * d->heads > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)d->tokens * (d->heads / c->kv_heads), most = spv_kv_max_length(c, s);
-  // what the kernels number in 31 bits: units of 256 rows x 128 keys and the rows of one sequence's dense copies ...
-  if ((rows + 255) / 256 * ((most + 127) / 128) * c->kv_heads > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
+  // what the kernels number in 31 bits: tiles of 128 rows x 128 keys and the rows of one sequence's dense copies ...
+  if ((rows + 255) / 256 * 2 * ((most + 127) / 128) * c->kv_heads > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
   if ((most + 127 > rows + 255 ? most + 127 : rows + 255) * c->kv_heads > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;
   // ... and tiles of 32 slots of all sequences
   if ((int64_t)s->batch * c->kv_heads * ((most + 31) / 32) > INT32_MAX / 2) return SPV_ERR_UNSUPPORTED;

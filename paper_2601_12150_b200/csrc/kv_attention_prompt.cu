@@ -15,8 +15,10 @@
 //                        keys in one buffer, two issuing threads: a block's chain of S, softmax and O was 6200 cycles a
 //                        tile, 208 us for 2 x 1501 tokens over 6001 slots, 32 heads of 128.)
 //   kv_prompt_join       units that were cut between CTAs.
-//   kv_prompt_weigh      weights: S^T = K Q^T by tiles of 128 keys, so that a key's scores are a thread's own and its
-//                        sum over the rows needs no other thread; 2^(z - lse) with the rows' lse from before.
+//   kv_prompt_weigh      weights: S^T = K Q^T by tiles of 128 keys, so that a key's scores are two threads' own and its
+//                        sum over the rows needs no others; 2^(z - lse) with the rows' lse from before.  Equal stretches
+//                        of the line of (key tile, row tile) here too: 752 key tiles on 296 places took three turns.
+//   kv_prompt_weigh_join key tiles that were cut.
 #include <type_traits>
 
 #include "kv_attention.cuh"
@@ -50,6 +52,9 @@ struct PromptArgs {
   float2* part_ml;                         // [CTA][2][256]
   Unit* units;                             // in the order of the line
   int* head;                               // [0] tiles of the line, then for each CTA the units its stretch begins and ends in
+  int* weigh_line;                         // [nb + 1]: key tiles x row tiles of the weights' kernel before each sequence
+  float* part_w;                           // [weighing CTA][2][128]
+  struct Tile* last_tile;                  // [weighing CTA]
   int32_t ctas;
 };
 
@@ -82,6 +87,13 @@ __device__ __forceinline__ int block_tiles(int len, int n, int group, int causal
   return max(1, (end + kKeys - 1) / kKeys);
 }
 
+// The weights' kernel: row tiles of 128 that see some key of the key tile `kt`: [first, all row tiles).
+__device__ __forceinline__ int first_row_tile(int len, int n, int group, int causal, int kt) {
+  if (!causal) return 0;
+  const int64_t row = ((int64_t)kt * kKeys - len + n) * group;       // the first that sees the first key
+  return row <= 0 ? 0 : (int)min((int64_t)n * group, row) / 128;
+}
+
 // Equal stretches of the line: the first `more` CTAs have per + 1 tiles, the others per.
 struct Share {
   int working, per, more;
@@ -99,10 +111,10 @@ struct Share {
 
 // One block: all units of the round in order, and where every CTA's stretch begins and ends.  A warp per sequence.
 __device__ void make_plan(const KvView& c, const PromptArgs& s) {
-  __shared__ int seq_units[kPrepThreads], seq_tiles[kPrepThreads];       // of the sequences of a batch of 256
-  __shared__ int base_units, base_tiles;
+  __shared__ int seq_units[kPrepThreads], seq_tiles[kPrepThreads], seq_weigh[kPrepThreads];   // of 256 sequences
+  __shared__ int base_units, base_tiles, base_weigh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) base_units = base_tiles = 0;
+  if (threadIdx.x == 0) base_units = base_tiles = base_weigh = 0;
   for (int b0 = 0; b0 < s.nb; b0 += kPrepThreads) {
     const int count = min(kPrepThreads, s.nb - b0);
     for (int pass = 0; pass < 2; ++pass) {
@@ -129,16 +141,26 @@ __device__ void make_plan(const KvView& c, const PromptArgs& s) {
           }
           per_head = at;
         }
-        if (!pass && lane == 0) {
-          seq_units[i] = units * c.kv_heads;
-          seq_tiles[i] = per_head * c.kv_heads;
+        if (!pass) {
+          int weigh = 0;
+          if (units)
+            for (int kt = lane; kt * kKeys < len; kt += 32)
+              weigh += (n * s.a.group + 127) / 128 - first_row_tile(len, n, s.a.group, s.a.causal, kt);
+          weigh = __reduce_add_sync(0xffffffffu, weigh);
+          if (lane == 0) {
+            seq_units[i] = units * c.kv_heads;
+            seq_tiles[i] = per_head * c.kv_heads;
+            seq_weigh[i] = weigh * c.kv_heads;
+          }
         }
       }
       __syncthreads();
       if (!pass) {
         if (threadIdx.x == 0) {
-          int u = base_units, t = base_tiles;
+          int u = base_units, t = base_tiles, w = base_weigh;
           for (int i = 0; i < count; ++i) {
+            s.weigh_line[b0 + i] = w;
+            w += seq_weigh[i];
             const int du = seq_units[i], dt = seq_tiles[i];
             seq_units[i] = u;
             seq_tiles[i] = t;
@@ -147,6 +169,8 @@ __device__ void make_plan(const KvView& c, const PromptArgs& s) {
           }
           base_units = u;
           base_tiles = t;
+          base_weigh = w;
+          s.weigh_line[b0 + count] = w;
         }
         __syncthreads();
       }
@@ -683,7 +707,7 @@ __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const Prom
   }
 }
 
-// ---- weights: grid (key tiles, key heads, sequences), two CTAs an SM ------------------------------------
+// ---- weights: two CTAs an SM, equal stretches of the line of (key tile, row tile) -----------------------
 constexpr int kWeighThreads = 320;         // eight warps of sums (two threads per key, half of the rows each), producer, issuer
 template <int D>
 struct WeighSmem {
@@ -696,34 +720,118 @@ struct WeighSmem {
   static constexpr int kTotal = oHalf + 512;
 };
 
+struct alignas(16) Tile {                  // 128 keys of a pair, and its row tiles' places on the line
+  int b, head, kt, len;
+  int n, first, line, count;
+};
+struct TileWalk {
+  int pos, end;
+  Tile t;
+};
+__device__ __forceinline__ void fill_tile(const KvView& c, const PromptArgs& s, Tile& t) {
+  t.first = first_row_tile(t.len, t.n, s.a.group, s.a.causal, t.kt);
+  t.count = (t.n * s.a.group + 127) / 128 - t.first;
+}
+// The tile that holds place `pos` of the line; a whole warp.
+__device__ __forceinline__ Tile find_tile(const KvView& c, const PromptArgs& s, int pos) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = s.nb - 1;               // the last sequence that begins at or before pos
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s.weigh_line[mid] <= pos) lo = mid;
+    else hi = mid - 1;
+  }
+  Tile t;
+  t.b = lo;
+  t.len = seq_len(c, s.b0 + lo);
+  t.n = seq_queries(s.a, s.b0 + lo);
+  const int begin = s.weigh_line[lo], per_head = (s.weigh_line[lo + 1] - begin) / c.kv_heads;
+  t.head = (pos - begin) / per_head;
+  int line = begin + t.head * per_head;
+  const int tiles = (t.len + kKeys - 1) / kKeys;
+  for (int k0 = 0; k0 < tiles; k0 += 32) {
+    t.kt = k0 + lane;
+    t.count = 0;
+    if (t.kt < tiles) fill_tile(c, s, t);
+    int inc = t.count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += x;
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, t.count && pos < line + inc);
+    if (hit) {
+      const int at = __ffs(hit) - 1;
+      t.line = line + inc - t.count;
+      t.line = __shfl_sync(0xffffffffu, t.line, at);
+      t.kt = k0 + at;
+      fill_tile(c, s, t);
+      return t;
+    }
+    line += __shfl_sync(0xffffffffu, inc, 31);
+  }
+  return t;                                // not reached: pos is on the line
+}
+// Row tiles [r0, r1) of tile w.t are next.
+__device__ __forceinline__ bool next_rows(const TileWalk& w, int& r0, int& r1) {
+  if (w.pos >= w.end) return false;
+  r0 = w.t.first + w.pos - w.t.line;
+  r1 = min(w.t.first + w.t.count, r0 + w.end - w.pos);
+  return true;
+}
+__device__ __forceinline__ void advance(const KvView& c, const PromptArgs& s, TileWalk& w, int rows) {
+  w.pos += rows;
+  if (w.pos >= w.end) return;              // (the tile may go on in the next CTA)
+  w.t.line += w.t.count;
+  if (++w.t.kt * kKeys >= w.t.len) {
+    w.t.kt = 0;
+    if (++w.t.head == c.kv_heads) {
+      w.t.head = 0;
+      do {                                 // w.pos < w.end: a sequence with tiles follows
+        ++w.t.b;
+        w.t.len = seq_len(c, s.b0 + w.t.b);
+        w.t.n = seq_queries(s.a, s.b0 + w.t.b);
+      } while (w.t.len == 0 || w.t.n == 0);
+    }
+  }
+  fill_tile(c, s, w.t);
+}
+
 template <int D>
 __global__ void __launch_bounds__(kWeighThreads, 2)
     kv_prompt_weigh(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const KvView c,
                     const PromptArgs s) {
   using L = WeighSmem<D>;
   constexpr int ST = L::kStages;
-  const int head = blockIdx.y, b = s.b0 + blockIdx.z, key0 = blockIdx.x * kKeys;
-  const int pair = blockIdx.z * c.kv_heads + head;
-  const int len = seq_len(c, b), n = seq_queries(s.a, b), rows = n * s.a.group;
-  if (key0 >= len) return;
-  // rows that see a key: those from (key - (len - n)) * group on, where the mask is causal
-  auto first_row = [&](int key) { return s.a.causal ? (int)max((int64_t)0, ((int64_t)key - len + n) * s.a.group) : 0; };
-  const int t0 = min(first_row(key0), rows) / 128, t1 = (rows + 127) / 128;
-  const int key = key0 + (threadIdx.x & 127);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::oBars);
   uint64_t* k_full = bars;
-  uint64_t* q_full = bars + 1;             // [ST] tile and row_stat
+  uint64_t* k_empty = bars + 1;            // the products with the key tile are done
+  uint64_t* q_full = bars + 2;             // [ST] tile and row_stat
   uint64_t* q_empty = q_full + ST;         // [ST] product done and row_stat read
   uint64_t* s_full = q_empty + ST;         // [2]
   uint64_t* s_empty = s_full + 2;          // [2]
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_empty + 2);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  __shared__ Tile s_first;
   uint32_t* status = c.status - 1;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // sequences without queries keep their weights
+  for (int b = s.b0 + blockIdx.x; b < s.b0 + s.nb; b += gridDim.x) {
+    if (seq_queries(s.a, b) > 0) continue;
+    const int len = seq_len(c, b);
+    for (int h = 0; h < c.kv_heads; ++h)
+      for (int x = threadIdx.x; x < len; x += kWeighThreads) {
+        const int64_t at = b * s.a.w_stride_b + h * s.a.w_stride_head + x;
+        s.a.w_out[at] = s.a.w_in ? s.a.w_in[at] : 0.0f;
+      }
+  }
+  const Share share(s.weigh_line[s.nb], gridDim.x);
+  if ((int)blockIdx.x >= share.working) return;
   if (threadIdx.x == 0) {
     mbar_init(k_full, 1);
+    mbar_init(k_empty, 1);
     for (int i = 0; i < ST; ++i) {
       mbar_init(q_full + i, 2);
       mbar_init(q_empty + i, 1 + 256);
@@ -739,100 +847,140 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
     tmem_alloc(tmem_slot, 256);
     tmem_relinquish();
   }
+  TileWalk w;
+  w.pos = share.begin(blockIdx.x);
+  w.end = share.begin(blockIdx.x + 1);
+  if (warp == 0) {
+    const Tile t = find_tile(c, s, w.pos);
+    if (lane == 0) s_first = t;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  w.t = s_first;
+  int r0, r1;
   if (warp == 8) {
-    if (lane == 0 && t0 < t1) {
-      mbar_expect_tx(k_full, L::kTile);
-      load_tile<D>(smem, &map_k, k_full, pair * s.keys_pad + key0);
-    }
-    for (int t = t0; t < t1; ++t) {
-      const uint32_t j = t - t0, st = j % ST;
-      mbar_wait(q_empty + st, ((j / ST) & 1) ^ 1, abort_flag, status, 0x4D00u);
+    uint32_t j = 0, tiles = 0;
+    for (; next_rows(w, r0, r1); advance(c, s, w, r1 - r0), ++tiles) {
+      const int pair = w.t.b * c.kv_heads + w.t.head;
+      if (tiles) mbar_wait(k_empty, (tiles - 1) & 1, abort_flag, status, 0x4D06u);
       if (lane == 0) {
-        mbar_expect_tx(q_full + st, L::kTile);
-        load_tile<D>(smem + L::oQ + st * L::kTile, &map_q, q_full + st, pair * s.rows_pad + t * 128);
+        mbar_expect_tx(k_full, L::kTile);
+        load_tile<D>(smem, &map_k, k_full, pair * s.keys_pad + w.t.kt * kKeys);
       }
-      reinterpret_cast<float4*>(smem + L::oStat + st * 512)[lane] =
-          reinterpret_cast<const float4*>(s.row_stat + (size_t)pair * s.rows_pad + t * 128)[lane];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_full + st);
-      __syncwarp();
+      for (int t = r0; t < r1; ++t, ++j) {
+        const uint32_t st = j % ST;
+        mbar_wait(q_empty + st, ((j / ST) & 1) ^ 1, abort_flag, status, 0x4D00u);
+        if (lane == 0) {
+          mbar_expect_tx(q_full + st, L::kTile);
+          load_tile<D>(smem + L::oQ + st * L::kTile, &map_q, q_full + st, pair * s.rows_pad + t * 128);
+        }
+        reinterpret_cast<float4*>(smem + L::oStat + st * 512)[lane] =
+            reinterpret_cast<const float4*>(s.row_stat + (size_t)pair * s.rows_pad + t * 128)[lane];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full + st);
+        __syncwarp();
+      }
+    }
+    // a wait that gave up may leave copies behind: they end before the CTA does
+    if (*abort_flag != 0u && lane == 0) {
+      for (int i = 0; i < 1 + ST; ++i) {
+        uint64_t* bar = i ? q_full + i - 1 : k_full;
+        for (int tries = 0; tries < 1000 && !mbar_try_wait_parked(bar, 0, 1000u) && !mbar_try_wait_parked(bar, 1, 1000u); ++tries) {
+        }
+      }
     }
   } else if (warp == 9) {
-    if (lane == 0 && t0 < t1) {
+    if (lane == 0) {
       constexpr uint32_t idesc = idesc_f16(128, 128, false);
       const uint64_t dk = smem_desc_sw128(smem_u32(smem));
-      mbar_wait(k_full, 0, abort_flag, status, 0x4D01u);
-      for (int t = t0; t < t1; ++t) {
-        const uint32_t j = t - t0, st = j % ST, sb = j & 1;
-        mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D02u);
-        mbar_wait(s_empty + sb, ((j >> 1) & 1) ^ 1, abort_flag, status, 0x4D03u);
-        tc_fence_after();
-        const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + st * L::kTile));
+      uint32_t j = 0, tiles = 0;
+      for (; next_rows(w, r0, r1); advance(c, s, w, r1 - r0), ++tiles) {
+        mbar_wait(k_full, tiles & 1, abort_flag, status, 0x4D01u);
+        for (int t = r0; t < r1; ++t, ++j) {
+          const uint32_t st = j % ST, sb = j & 1;
+          mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D02u);
+          mbar_wait(s_empty + sb, ((j >> 1) & 1) ^ 1, abort_flag, status, 0x4D03u);
+          tc_fence_after();
+          const uint64_t dq = smem_desc_sw128(smem_u32(smem + L::oQ + st * L::kTile));
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);
-          mma_ss(tmem + sb * 128, dk + off, dq + off, idesc, kk != 0);
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint64_t off = (uint64_t)(kk / 4 * 1024 + kk % 4 * 2);
+            mma_ss(tmem + sb * 128, dk + off, dq + off, idesc, kk != 0);
+          }
+          tc_commit(s_full + sb);
+          tc_commit(q_empty + st);
         }
-        tc_commit(s_full + sb);
-        tc_commit(q_empty + st);
+        tc_commit(k_empty);
       }
     }
   } else {
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const int half = warp >> 2;              // its rows of a tile: 64 half ..
-    const int first = first_row(key);
-    const float unit = t0 < t1 ? s.refs[pair].x : 0.0f;
-    float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
-    for (int t = t0; t < t1; ++t) {
-      const uint32_t j = t - t0, st = j % ST, sb = j & 1;
-      mbar_wait(s_full + sb, (j >> 1) & 1, abort_flag, status, 0x4D04u);
-      mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D05u);     // row_stat
-      __syncwarp();
-      tc_fence_after();
-      const float4* stat = reinterpret_cast<const float4*>(smem + L::oStat + st * 512);
-      const float f = s.q_factor[(size_t)pair * (s.rows_pad / 128) + t] * unit;
-      const float2 f2 = make_float2(f, f);
-      const int hidden = first - t * 128;                 // rows of the tile that do not see this thread's key
-      const bool mask = __any_sync(0xffffffffu, hidden > 0);
+    float* other = reinterpret_cast<float*>(smem + L::oHalf);
+    uint32_t j = 0;
+    for (; next_rows(w, r0, r1); advance(c, s, w, r1 - r0)) {
+      const int pair = w.t.b * c.kv_heads + w.t.head, key = w.t.kt * kKeys + (threadIdx.x & 127);
+      // the first row that sees this thread's key
+      const int first = s.a.causal ? (int)max((int64_t)0, ((int64_t)key - w.t.len + w.t.n) * s.a.group) : 0;
+      const float unit = s.refs[pair].x;
+      float2 sum0 = make_float2(0.0f, 0.0f), sum1 = make_float2(0.0f, 0.0f);
+      for (int t = r0; t < r1; ++t, ++j) {
+        const uint32_t st = j % ST, sb = j & 1;
+        const float f = s.q_factor[(size_t)pair * (s.rows_pad / 128) + t] * unit;
+        const float2 f2 = make_float2(f, f);
+        mbar_wait(s_full + sb, (j >> 1) & 1, abort_flag, status, 0x4D04u);
+        mbar_wait(q_full + st, (j / ST) & 1, abort_flag, status, 0x4D05u);     // row_stat
+        __syncwarp();
+        tc_fence_after();
+        const float4* stat = reinterpret_cast<const float4*>(smem + L::oStat + st * 512);
+        const int hidden = first - t * 128;                 // rows of the tile that do not see this thread's key
+        const bool mask = __any_sync(0xffffffffu, hidden > 0);
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int h = 2 * half + g;
-        uint32_t z[32];
-        tmem_ld32(tmem + sb * 128 + lane_off + 32 * h, z);
-        tc_wait_ld();
+        for (int g = 0; g < 2; ++g) {
+          const int h = 2 * half + g;
+          uint32_t z[32];
+          tmem_ld32(tmem + sb * 128 + lane_off + 32 * h, z);
+          tc_wait_ld();
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-          const float4 nl = stat[8 * h + i / 4];
-          const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), f2, make_float2(nl.x, nl.y));
-          const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), f2, make_float2(nl.z, nl.w));
-          float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y)), p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
-          if (mask) {
-            const int at = 32 * h + i;
-            if (at < hidden) p0.x = 0.0f;
-            if (at + 1 < hidden) p0.y = 0.0f;
-            if (at + 2 < hidden) p1.x = 0.0f;
-            if (at + 3 < hidden) p1.y = 0.0f;
+          for (int i = 0; i < 32; i += 4) {
+            const float4 nl = stat[8 * h + i / 4];
+            const float2 a0 = __ffma2_rn(make_float2(__uint_as_float(z[i]), __uint_as_float(z[i + 1])), f2, make_float2(nl.x, nl.y));
+            const float2 a1 = __ffma2_rn(make_float2(__uint_as_float(z[i + 2]), __uint_as_float(z[i + 3])), f2, make_float2(nl.z, nl.w));
+            float2 p0 = make_float2(exp2_fast(a0.x), exp2_fast(a0.y)), p1 = make_float2(exp2_fast(a1.x), exp2_fast(a1.y));
+            if (mask) {
+              const int at = 32 * h + i;
+              if (at < hidden) p0.x = 0.0f;
+              if (at + 1 < hidden) p0.y = 0.0f;
+              if (at + 2 < hidden) p1.x = 0.0f;
+              if (at + 3 < hidden) p1.y = 0.0f;
+            }
+            sum0 = __fadd2_rn(sum0, p0);
+            sum1 = __fadd2_rn(sum1, p1);
           }
-          sum0 = __fadd2_rn(sum0, p0);
-          sum1 = __fadd2_rn(sum1, p1);
+        }
+        tc_fence_before();
+        mbar_arrive(s_empty + sb);
+        mbar_arrive(q_empty + st);
+      }
+      const float sum = (sum0.x + sum0.y) + (sum1.x + sum1.y);
+      if (half) other[threadIdx.x & 127] = sum;
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      if (!half) {
+        const float all = sum + other[threadIdx.x];
+        if (r0 == w.t.first && r1 == w.t.first + w.t.count) {
+          if (key < w.t.len) {
+            const int64_t at = (s.b0 + w.t.b) * s.a.w_stride_b + w.t.head * s.a.w_stride_head + key;
+            s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + all;
+          }
+        } else {
+          s.part_w[(2 * blockIdx.x + (r0 == w.t.first ? 1 : 0)) * 128 + threadIdx.x] = all;
         }
       }
-      tc_fence_before();
-      mbar_arrive(s_empty + sb);
-      mbar_arrive(q_empty + st);
+      asm volatile("bar.sync 1, 256;" ::: "memory");        // `other` may be written again
     }
-    float* other = reinterpret_cast<float*>(smem + L::oHalf);
-    const float sum = (sum0.x + sum0.y) + (sum1.x + sum1.y);
-    if (half) other[threadIdx.x & 127] = sum;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (!half && key < len) {
-      const int64_t at = b * s.a.w_stride_b + head * s.a.w_stride_head + key;
-      s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + (sum + other[threadIdx.x]);
-    }
+    if (threadIdx.x == 0) s.last_tile[blockIdx.x] = w.t;
   }
   tc_fence_before();
   __syncthreads();
@@ -840,12 +988,29 @@ __global__ void __launch_bounds__(kWeighThreads, 2)
   if (warp == 9) tmem_dealloc(tmem, 256);
 }
 
+// Key tiles that were cut between weighing CTAs: the one that begins in this CTA and goes on, in the order of the rows.
+__global__ void __launch_bounds__(128) kv_prompt_weigh_join(const KvView c, const PromptArgs s, int ctas) {
+  const Share share(s.weigh_line[s.nb], ctas);
+  if ((int)blockIdx.x >= share.working) return;
+  const Tile t = s.last_tile[blockIdx.x];
+  const int c0 = share.owner(t.line), c1 = share.owner(t.line + t.count - 1);
+  if (c0 != (int)blockIdx.x || c0 == c1) return;
+  const int key = t.kt * kKeys + threadIdx.x;
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int i = c0; i <= c1; ++i) sum += s.part_w[(2 * i + (i == c0 ? 1 : 0)) * 128 + threadIdx.x];
+  if (key < t.len) {
+    const int64_t at = (s.b0 + t.b) * s.a.w_stride_b + t.head * s.a.w_stride_head + key;
+    s.a.w_out[at] = (s.a.w_in ? s.a.w_in[at] : 0.0f) + sum;
+  }
+}
+
 // ---- host --------------------------------------------------------------------------------------------
 constexpr size_t kRoundBytes = (size_t)2 << 30;      // dense copies of one round of sequences, one sequence at least
 
 struct Plan {
   int rows_pad, keys_pad, round;                     // sequences of a round
-  size_t q16, k16, v16, q_factor, refs, row_stat, part_o, part_ml, units, head, total;
+  size_t q16, k16, v16, q_factor, refs, row_stat, part_o, part_ml, units, head, weigh_line, part_w, last_tile, total;
 };
 Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d) {
   Plan w;
@@ -858,6 +1023,9 @@ Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d
   // rows of the dense copies are numbered in 31 bits
   const size_t most = (size_t)INT32_MAX / ((size_t)c->kv_heads * (w.keys_pad > w.rows_pad ? w.keys_pad : w.rows_pad));
   if (round > most) round = most;
+  // ... and so are the tiles of 128 rows x 128 keys
+  const size_t tiles = (size_t)c->kv_heads * (w.keys_pad / 128) * (w.rows_pad / 128);
+  if (round > INT32_MAX / 2 / tiles) round = INT32_MAX / 2 / tiles;
   if (round < 1) round = 1;
   if (round > (size_t)q->batch) round = q->batch;
   w.round = (int)round;
@@ -878,6 +1046,9 @@ Plan plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_desc* d
   w.part_ml = take((size_t)kMaxSms * 2 * kRowsUnit * sizeof(float2));
   w.units = take(pairs * (w.rows_pad / kRowsUnit) * sizeof(Unit));
   w.head = take((1 + 2 * kMaxSms) * sizeof(int));
+  w.weigh_line = take((round + 1) * sizeof(int));
+  w.part_w = take((size_t)2 * kMaxSms * 2 * 128 * sizeof(float));
+  w.last_tile = take(2 * kMaxSms * sizeof(Tile));
   w.total = at;
   return w;
 }
@@ -899,6 +1070,9 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
   s.part_ml = (float2*)(base + w.part_ml);
   s.units = (Unit*)(base + w.units);
   s.head = (int*)(base + w.head);
+  s.weigh_line = (int*)(base + w.weigh_line);
+  s.part_w = (float*)(base + w.part_w);
+  s.last_tile = (Tile*)(base + w.last_tile);
   const uint64_t strides[1] = {(uint64_t)D * 2};
   const uint32_t box[2] = {64, 128};
   const uint64_t q_dims[2] = {(uint64_t)D, (uint64_t)w.round * view.kv_heads * w.rows_pad};
@@ -928,8 +1102,9 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
     kv_prompt_join<D><<<dim3(ctas, kRowsUnit / 16), 256, 0, stream>>>(view, s, ctas);
     launches += 3;
     if (a.w_out) {
-      kv_prompt_weigh<D><<<dim3(w.keys_pad / kKeys, view.kv_heads, s.nb), kWeighThreads, weigh_bytes, stream>>>(mq, mk, view, s);
-      ++launches;
+      kv_prompt_weigh<D><<<2 * ctas, kWeighThreads, weigh_bytes, stream>>>(mq, mk, view, s);
+      kv_prompt_weigh_join<<<2 * ctas, 128, 0, stream>>>(view, s, 2 * ctas);
+      launches += 2;
     }
   }
   return spv_launch_ok(ctx, launches);
