@@ -285,7 +285,8 @@ typedef struct {
   int32_t block;                     /* tokens of a page: 16, 32, 64 or 128                      */
   int32_t format;                    /* SPV_KV_INT8 | SPV_KV_E4M3                                */
   void *k, *v;                       /* device, 8-bit codes [pages, kv_heads, block, head_dim]   */
-  float *k_scale, *v_scale;          /* device [pages, kv_heads], positive and finite            */
+  float *k_scale, *v_scale;          /* device [pages, kv_heads], positive and finite;
+                                        kv_cache_append writes powers of two               */
 } spv_kv_cache;
 
 typedef struct {
@@ -331,7 +332,12 @@ int32_t kv_cache_append(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_se
  * weights_out: optional fp32 [batch, kv_heads, >= max_length] with strides:
  *   weights_out[j] = weights_in[j] + sum of softmax_j over the queries and the heads of a key head,
  * j < L (weights_in NULL: 0; may be weights_out itself: it then accumulates).  Same strides.
- * Sums are in fp32 in a fixed order: the same call gives the same bits. */
+ * Sums are in fp32 in a fixed order: the same call gives the same bits.  Probabilities are rounded
+ * to fp16 for the product with the values.  Calls with more than 32 queries x heads to a key head
+ * work on fp16 copies of keys and values, exact where scales are powers of two (within 2^24 of one
+ * another in a sequence), else rounded (2^-11); their workspace holds these copies, 4 * head_dim
+ * bytes a slot and key head for up to 2 GB of sequences at a time (one sequence at least).
+ * weights_in is weights_out or does not overlap it. */
 typedef struct {
   int32_t tokens, heads;
   int32_t dtype;                     /* SPV_BF16 | SPV_FP16                                      */

@@ -483,8 +483,12 @@ class Context:
     def _kv_scratch(self, nbytes, workspace, stream):
         """The caller's workspace, or one from torch's allocator in the order of the call's stream: a captured
         graph then owns its own, and calls on two streams do not share one."""
-        if workspace is not None or nbytes == 0:
+        if workspace is not None:
+            _need(workspace.dtype is self._torch.uint8 and workspace.is_contiguous() and workspace.get_device() == self._index,
+                  "workspace: contiguous uint8 on the context's device")
             return workspace
+        if nbytes == 0:
+            return None
         if stream is None:
             return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
         with self._torch.cuda.stream(stream):

@@ -658,53 +658,61 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// ---- units that were cut: grid (CTA, 16 rows) ---------------------------------------------------------
+// ---- units that were cut: grid (CTA, 256 / kJoinRows) ---------------------------------------------------
 template <int D>
 __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const PromptArgs s, int ctas) {
+  constexpr int kLanes = D / 4, kJoinRows = 256 / kLanes;        // a thread has four values of a row
   const Share share(s.head[0], ctas);
   if ((int)blockIdx.x >= share.working) return;
   const Unit d = s.units[s.head[2 + 2 * blockIdx.x]];      // the last one that begins here
   const int c0 = share.owner(d.line), c1 = share.owner(d.line + d.tiles - 1), rows = d.n * s.a.group;
   if (c0 != (int)blockIdx.x || c0 == c1) return;
   const int pair = d.b * c.kv_heads + d.head;
-  const float2 ref = s.refs[pair];
-  constexpr int kLanes = D / 4;
-  for (int r = threadIdx.x / kLanes; r < 16; r += 256 / kLanes) {
-    const int in = blockIdx.y * 16 + r, row = d.unit * kRowsUnit + in, col = threadIdx.x % kLanes * 4;
-    float top = -INFINITY;
-    for (int i = c0; i <= c1; ++i) top = fmaxf(top, s.part_ml[(size_t)(2 * i + (i == c0)) * kRowsUnit + in].x);
-    float den = 0.0f;
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int i = c0; i <= c1; ++i) {
-      const size_t slot = (size_t)(2 * i + (i == c0)) * kRowsUnit + in;
-      const float2 ml = s.part_ml[slot];
-      if (ml.y > 0.0f || ml.y != ml.y) {                   // without a key nothing was written
-        const float f = exp2_fast(ml.x - (top == -INFINITY ? 0.0f : top));
-        const float4 v = *reinterpret_cast<const float4*>(s.part_o + slot * D + col);
-        den = fmaf(ml.y, f, den);
-        sum.x = fmaf(v.x, f, sum.x);
-        sum.y = fmaf(v.y, f, sum.y);
-        sum.z = fmaf(v.z, f, sum.z);
-        sum.w = fmaf(v.w, f, sum.w);
+  const int in = blockIdx.y * kJoinRows + threadIdx.x / kLanes, row = d.unit * kRowsUnit + in, col = threadIdx.x % kLanes * 4;
+  float top = -INFINITY, den = 0.0f;
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  // four pieces at a time: their loads do not wait for one another
+  for (int i0 = c0; i0 <= c1; i0 += 4) {
+    float2 ml[4];
+    float4 v[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      ml[x] = make_float2(-INFINITY, 0.0f);
+      if (i0 + x <= c1) {
+        const size_t slot = (size_t)(2 * (i0 + x) + (i0 + x == c0)) * kRowsUnit + in;
+        ml[x] = s.part_ml[slot];
+        v[x] = *reinterpret_cast<const float4*>(s.part_o + slot * D + col);
       }
     }
-    const bool some = den > 0.0f || den != den;
-    const bool real = row < rows;
-    if (real) {
-      const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
-      const float inv = some ? ref.y / den : 0.0f;
-      uint2 u;
-      if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv));
-      else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv));
-      *reinterpret_cast<uint2*>(s.a.o + (s.b0 + d.b) * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + col) = u;
-      if (col == 0 && s.a.lse)
-        s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    const float next = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+    const float ref = next == -INFINITY ? 0.0f : next, old = exp2_fast(top - ref);
+    den *= old;
+    sum = make_float4(sum.x * old, sum.y * old, sum.z * old, sum.w * old);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (ml[x].y > 0.0f || ml[x].y != ml[x].y) {          // without a key nothing was written
+        const float f = exp2_fast(ml[x].x - ref);
+        den = fmaf(ml[x].y, f, den);
+        sum.x = fmaf(v[x].x, f, sum.x);
+        sum.y = fmaf(v[x].y, f, sum.y);
+        sum.z = fmaf(v[x].z, f, sum.z);
+        sum.w = fmaf(v[x].w, f, sum.w);
+      }
     }
-    if (col == 0) {
-      s.row_stat[(size_t)pair * s.rows_pad + row] = real && some ? -(top + log2f(den)) : -INFINITY;
-    }
+    top = next;
   }
+  const bool some = den > 0.0f || den != den, real = row < rows;
+  if (real) {
+    const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
+    const float inv = some ? s.refs[pair].y / den : 0.0f;
+    uint2 u;
+    if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv));
+    else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv));
+    *reinterpret_cast<uint2*>(s.a.o + (s.b0 + d.b) * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + col) = u;
+    if (col == 0 && s.a.lse)
+      s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
+  }
+  if (col == 0) s.row_stat[(size_t)pair * s.rows_pad + row] = real && some ? -(top + log2f(den)) : -INFINITY;
 }
 
 // ---- weights: two CTAs an SM, equal stretches of the line of (key tile, row tile) -----------------------
@@ -1099,7 +1107,7 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
     s.nb = seqs->batch - b0 < w.round ? seqs->batch - b0 : w.round;
     kv_prompt_prepare<FMT, D><<<dim3(key_chunks + row_chunks + 1, view.kv_heads, s.nb), kPrepThreads, 0, stream>>>(view, s, key_chunks);
     kv_prompt_attend<D><<<ctas, kAttendThreads, attend_bytes, stream>>>(mq, mk, mv, view, s);
-    kv_prompt_join<D><<<dim3(ctas, kRowsUnit / 16), 256, 0, stream>>>(view, s, ctas);
+    kv_prompt_join<D><<<dim3(ctas, kRowsUnit * D / 1024), 256, 0, stream>>>(view, s, ctas);
     launches += 3;
     if (a.w_out) {
       kv_prompt_weigh<D><<<2 * ctas, kWeighThreads, weigh_bytes, stream>>>(mq, mk, view, s);

@@ -624,7 +624,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
         } else {
           const int i = row / s.a.group, head = p.head * s.a.group + row % s.a.group;
           if (i < p.n) {
-            const float f = m[t][e] == -INFINITY ? 0.0f : vref / l[t][e];
+            const float f = l[t][e] == 0.0f ? 0.0f : vref / l[t][e];         // (a NaN stays one)
             uint16_t* out = s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + head * s.a.o_stride_head + r * kMine;
 #pragma unroll
             for (int j = 0; j < kSteps; j += 4) {
@@ -639,7 +639,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
             if (r == 0) {
               if (s.a.lse)
                 s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + head] =
-                    m[t][e] == -INFINITY ? -INFINITY : (m[t][e] + log2f(l[t][e])) * 0.6931471805599453f;
+                    l[t][e] == 0.0f ? -INFINITY : (m[t][e] + log2f(l[t][e])) * 0.6931471805599453f;
               s.pair_ml[pair + row] = make_float2(m[t][e], l[t][e]);
             }
           }
@@ -734,11 +734,11 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
     for (int row = warp; row < rows; row += kFinishThreads / 32) {
       const float2 ml = c0 == c1 ? s.pair_ml[pair + row] : joined(s, workers, c0, c1, row);
       if (lane == 0) {
-        stat[row] = make_float2(ml.x == -INFINITY ? 0.0f : ml.x, ml.x == -INFINITY ? 0.0f : 1.0f / ml.y);
+        stat[row] = make_float2(ml.x == -INFINITY ? 0.0f : ml.x, ml.y == 0.0f ? 0.0f : 1.0f / ml.y);
         if (c0 != c1 && p.kt0 == 0 && s.a.lse) {
           const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
           s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + h] =
-              ml.x == -INFINITY ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
+              ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
         }
       }
     }

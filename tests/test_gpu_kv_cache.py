@@ -203,7 +203,7 @@ def test_read(ctx, fmt, out_type, block, dim):
 
 
 # ---- attention ---------------------------------------------------------------------------------
-def bounds(o, spread, reach, vmax, dim, length, dtype):
+def bounds(o, spread, reach, vmax, dim, length, dtype, rounded=False):
     """|computed - exact| at most, element by element.
     Logits: products of a query and a code are exact in fp32; their sum of `dim` terms is off by at most
     dim * 2^-23 * sum|q k| (tensor-core sums may truncate: 2^-23, not 2^-24), the scale and the shift by the maximum
@@ -213,16 +213,22 @@ def bounds(o, spread, reach, vmax, dim, length, dtype):
     it is below 2^-14 of the largest, 2^-25 of the largest, for each key.
     The sum over the keys in fp32: length * 2^-23 of sum p |v| at most, and far less in blocks: 64 terms at a time,
     the blocks' sums one after the other: (64 + length / 64) * 2^-23.
-    The result is rounded to its type: eps / 2 of it (and half the smallest subnormal)."""
+    The result is rounded to its type: eps / 2 of it (and half the smallest subnormal).
+    rounded: scales that are no powers of two, and many queries: keys and values are code * scale rounded to fp16, half a
+    step of it, 2^-11 of each.  A logit is then off by 2^-11 of sum|q k| more, p by twice that (exp(2 x) - 1 <= 2.1 x for the
+    x that occur), and sum p |v| by 2^-11."""
     dz = (dim + 6) * 2.0 ** -23 * reach
-    rel = 2 * dz + 2.0 ** -20 + 2.0 ** -11 + (64 + length / 64) * 2.0 ** -23
+    if rounded:
+        dz = 1.05 * (dz + 2.0 ** -11 * reach)
+        spread = spread * (1 + 2.0 ** -11)
+    rel = 2 * dz + (2.0 ** -11 if rounded else 0.0) + 2.0 ** -20 + 2.0 ** -11 + (64 + length / 64) * 2.0 ** -23
     eps = torch.finfo(ref.TORCH_TYPE[dtype]).eps
     tiny = torch.finfo(ref.TORCH_TYPE[dtype]).smallest_normal * eps
     return rel[..., None] * spread * (1 + eps) + length * 2.0 ** -25 * vmax[..., None] + eps / 2 * np.abs(o) + tiny
 
 
 def run_attention(ctx, rng, lengths, tokens, counts, heads, kv_heads, dim, block, fmt, dtype, causal, weights=True,
-                  scale=0.0, qscale=1.5, state=None):
+                  scale=0.0, qscale=1.5, state=None, rounded=False):
     B = len(lengths)
     cache, pool, table, dtable, dlen = state or filled(ctx, rng, lengths, kv_heads, dim, block, fmt, dtype)
     q = normals(rng, (B, tokens, heads, dim), dtype, qscale)
@@ -247,19 +253,19 @@ def run_attention(ctx, rng, lengths, tokens, counts, heads, kv_heads, dim, block
         n = tokens if counts is None else counts[b]
         o, l, w, spread, reach, vmax = ref.attention(pool, table[b], q[b].double().numpy(), length, n, heads, kv_heads,
                                                      causal, sc)
-        lim = bounds(o, spread, reach, vmax, dim, max(length, 1), dtype)
+        lim = bounds(o, spread, reach, vmax, dim, max(length, 1), dtype, rounded)
         err = np.abs(got[b, :n, :heads] - o)
         assert np.all(err <= lim), (b, length, n, float((err / lim).max()))
         assert np.all(got[b, n:, :heads] == 7.0) and np.all(glse[b, n:] == 7.0)
         some = np.isfinite(l)
         assert np.array_equal(np.isfinite(glse[b, :n]), some) and np.all(glse[b, :n][~some] == -np.inf)
-        dz = (dim + 6) * 2.0 ** -23 * reach
+        dz = ((dim + 6) * 2.0 ** -23 + (1.05 * 2.0 ** -11 if rounded else 0.0)) * reach
         lim = 2 * dz + 2.0 ** -20 + (64 + length / 64) * 2.0 ** -23 + 2.0 ** -22 * np.abs(np.where(some, l, 0.0))
         assert np.all(np.abs(np.where(some, glse[b, :n] - np.where(some, l, 0.0), 0.0)) <= lim)
         if weights:
             # every probability from its logit and the log-sum, both off by dz; then sums of n * group terms in fp32
             worst = float(reach.max()) if reach.size else 0.0
-            rel = 3 * (dim + 6) * 2.0 ** -23 * worst + 2.0 ** -19 + (64 + length / 64 + n * heads // kv_heads) * 2.0 ** -23
+            rel = 3 * ((dim + 6) * 2.0 ** -23 + (1.05 * 2.0 ** -11 if rounded else 0.0)) * worst + 2.0 ** -19 + (64 + length / 64 + n * heads // kv_heads) * 2.0 ** -23
             rel += 2.0 ** -22 * float(np.abs(l[some]).max()) if some.any() else 0.0
             want = win[b, :, :length] + w
             assert np.all(np.abs(gw[b, :, :length] - want) <= rel * w + 2.0 ** -24 * np.abs(want) + 1e-37), (b, length)
@@ -557,6 +563,80 @@ def test_bad_pages_and_lengths_are_latched(ctx):
     run_attention(ctx, rng, [70, 40], 3, None, 4, 2, 64, 16, "int8", "bf16", True, state=(cache, pool, table, dtable, dlen))
 
 
+@pytest.mark.parametrize("tokens", [1, 6, 100])
+def test_non_finite_queries_stay_in_their_rows(ctx, tokens):
+    """NaN and infinities in one query: its own output is NaN, every other is within its bound.  (Not bit for bit what
+    it is without them: a score of one query that renews its maximum renews those of its neighbours, and a probability
+    is rounded relative to the maximum that is in force.)"""
+    rng = np.random.default_rng(17)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [3000, 200], 2, 64, 32, "e4m3", "bf16")
+    q = normals(rng, (2, tokens, 8, 64), "bf16")
+    exact = [ref.attention(pool, table[b], q[b].double().numpy(), n, tokens, 8, 2, True, 0.125) for b, n in enumerate([3000, 200])]
+    for value in (float("nan"), float("inf"), -float("inf")):
+        bad = q.clone()
+        bad[0, tokens - 1, 3, 5] = value
+        got = ctx.kv_cache_attention(cache, bad.to(ctx.device), dtable, dlen).cpu().double().numpy()
+        ctx.check()
+        assert np.isnan(got[0, tokens - 1, 3]).all()
+        for b, (o, _, _, spread, reach, vmax) in enumerate(exact):
+            fine = np.abs(got[b] - o) <= bounds(o, spread, reach, vmax, 64, [3000, 200][b], "bf16")
+            if b == 0:
+                fine[tokens - 1, 3] = True
+            assert fine.all()
+
+
+def test_kernel_classes_and_workspaces(ctx):
+    """The calls show up in the per-class timing; a workspace of the caller's gives the same bits."""
+    rng = np.random.default_rng(18)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [400], 1, 64, 16, "int8", "bf16")
+    w = torch.zeros((1, 1, 400), device=ctx.device)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=ctx.device)
+    ctx.profile(True)
+    for tokens in (1, 50):
+        q = normals(rng, (1, tokens, 2, 64), "bf16").to(ctx.device)
+        one = ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w)
+        w2 = torch.zeros_like(w)
+        two = ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w2, workspace=ws, max_length=400)
+        assert torch.equal(one, two) and torch.equal(w, w2)
+    ctx.kv_cache_evict(cache, w, dtable, dlen, 100, workspace=ws)
+    stat = ctx.profile_read()
+    ctx.profile(False)
+    ctx.check()
+    assert stat["kv_attn"]["launches"] == 4 and stat["kv_cache"]["launches"] == 1
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_scales_that_are_no_powers_of_two(ctx, fmt, tokens):
+    """A cache that something else quantised: any positive scales.  Attention and read-back take them as they are;
+    eviction quantises anew, within half a step of the new scale (and of fp32's rounding of code * scale)."""
+    rng = np.random.default_rng(19)
+    n, block, dim = 300, 32, 64
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [n], 2, dim, block, fmt, "bf16")
+    for m in "kv":
+        f = torch.from_numpy(rng.uniform(0.5, 3.0, (cache.pages, 2)).astype(np.float32)).to(ctx.device)
+        t = getattr(cache, m + "_scale")
+        t.copy_(torch.where(torch.isfinite(t), t * f, t))
+    pool = ref.Pool.of(cache)
+    run_attention(ctx, rng, [n], tokens, None, 4, 2, dim, block, fmt, "bf16", True, state=(cache, pool, table, dtable, dlen),
+                  rounded=tokens > 16)
+    w = torch.from_numpy(rng.random((1, 2, n)).astype(np.float32)).to(ctx.device)
+    kept, nlen, _ = ctx.kv_cache_evict(cache, w, dtable, dlen, 100, 0, 5)
+    ctx.check()
+    new = ref.Pool.of(cache)
+    for h in range(2):
+        slots = kept[0, h].tolist()
+        for m in "kv":
+            was, now = pool.rows(m, table[0], slots, h), new.rows(m, table[0], np.arange(100), h)
+            for j in range(0, 100, block):
+                s = new.scale[m][table[0][j // block], h]
+                a = np.abs(was[j:j + block]).max()
+                assert ref.scale_of(a * (1 - 1e-6), fmt) <= s <= ref.scale_of(a * (1 + 1e-6), fmt)
+                # int8: half a step; e4m3: half a unit in the last of four digits, or half of 2^-9
+                half = 0.5 * s if fmt == "int8" else np.maximum(np.abs(was[j:j + block]) * 2.0 ** -4, s * 2.0 ** -10)
+                assert np.all(np.abs(now[j:j + block] - was[j:j + block]) <= half * (1 + 1e-5) + 1e-6 * np.abs(was[j:j + block]))
+
+
 @pytest.mark.parametrize("tokens", [1, 100])
 def test_two_captured_graphs(ctx, tokens):
     """A step captured twice, for two sequences' buffers, replayed in turn: each equals the direct call."""
@@ -649,6 +729,7 @@ def test_refusals(ctx):
     refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, max_length=10 ** 6))
     refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, counts=dlen[:1]))
     refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, weights_out=w, workspace=small[:128]), spv.ERR_WORKSPACE)
+    refused(lambda: ctx.kv_cache_attention(cache, q, dtable, dlen, workspace=torch.empty(1 << 24, dtype=torch.uint8)))
     odd = torch.zeros(2 * 4 * 65 + 8, dtype=torch.bfloat16, device=ctx.device)
     refused(lambda: ctx.kv_cache_attention(cache, odd[1:513].view(2, 1, 4, 64), dtable, dlen), spv.ERR_ALIGNMENT)
     refused(lambda: ctx.kv_cache_attention(cache, odd[:2 * 4 * 65].view(2, 1, 4, 65)[..., :64], dtable, dlen), spv.ERR_ALIGNMENT)
