@@ -268,6 +268,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
   auto load = [&](int tile) {
 #pragma unroll
     for (int i = 0; i < kSelItems; ++i) {
+      if (tile + i * kSelThreads >= m) break;             // (uniform, as in the loops below)
       const int j = tile + i * kSelThreads + threadIdx.x;
       key[i] = j < m ? rank_key(__ldg(w + j)) : 0u;
     }
@@ -283,9 +284,11 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
     for (int tile = 0; tile < m; tile += kSelTile) {
       if (m > kSelTile) load(tile);
 #pragma unroll
-      for (int i = 0; i < kSelItems; ++i)
+      for (int i = 0; i < kSelItems; ++i) {
+        if (tile + i * kSelThreads >= m) break;
         if (tile + i * kSelThreads + (int)threadIdx.x < m && (key[i] & himask) == prefix)
           atomicAdd(&hist[key[i] >> shift & (bins - 1)], 1);
+      }
     }
     __syncthreads();
     // the bin of the k-th largest: thread t sums the bins from the top down, `per` of them
@@ -321,6 +324,10 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
     if (m > kSelTile) load(tile);
 #pragma unroll
     for (int i = 0; i < kSelItems; ++i) {
+      if (tile + i * kSelThreads >= m) {
+        if (lane == 0) counts[i * 32 + warp] = make_int2(0, 0);
+        continue;
+      }
       const bool valid = tile + i * kSelThreads + (int)threadIdx.x < m;
       const uint32_t gt = __ballot_sync(0xffffffffu, valid && key[i] > thr), eq = __ballot_sync(0xffffffffu, valid && key[i] == thr);
       if (lane == 0) counts[i * 32 + warp] = make_int2(__popc(gt), __popc(eq));
@@ -344,6 +351,7 @@ __global__ void __launch_bounds__(kSelThreads) kv_select_kernel(KvView c, EvictA
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSelItems; ++i) {
+      if (tile + i * kSelThreads >= m) break;
       const int j = tile + i * kSelThreads + threadIdx.x;
       const bool gt = j < m && key[i] > thr, eq = j < m && key[i] == thr;
       const uint32_t lower = (1u << lane) - 1u;
