@@ -489,10 +489,14 @@ class Context:
             return workspace
         if nbytes == 0:
             return None
+        return self._kv_new(self._torch.empty, nbytes, self._torch.uint8, stream)
+
+    def _kv_new(self, make, shape, dtype, stream):
+        """A tensor made in the order of the call's stream."""
         if stream is None:
-            return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+            return make(shape, dtype=dtype, device=self.device)
         with self._torch.cuda.stream(stream):
-            return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
+            return make(shape, dtype=dtype, device=self.device)
 
     def _kv_stream(self, stream):
         if stream is not None:
@@ -537,17 +541,17 @@ class Context:
         shape = q.shape
         B, n, H, d = shape
         if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+            out = self._kv_new(torch.empty, shape, q.dtype, stream)
         o_strides = out.stride()
         _need(out.dtype is q.dtype and out.shape == shape and o_strides[3] == 1 and out.get_device() == self._index and
-              _apart(o_strides, shape), "out: as q, no two elements at one place")
+              (out.is_contiguous() or _apart(o_strides, shape)), "out: as q, no two elements at one place")
         limit = page_table.shape[1] * cache.block
         wb = wh = w_in_at = w_out_at = lse_at = 0
         if weights_out is not None:
             self._kv_weights(cache, weights_out, B)
             wb, wh, _ = weights_out.stride()
             limit = min(limit, weights_out.shape[2])
-            _need(_apart((wb, wh, 1), weights_out.shape), "weights_out: no two elements at one place")
+            _need(weights_out.is_contiguous() or _apart((wb, wh, 1), weights_out.shape), "weights_out: no two elements at one place")
             w_out_at = weights_out.data_ptr()
         if weights_in is not None:
             _need(weights_out is not None, "weights_in: only with weights_out")
@@ -593,11 +597,11 @@ class Context:
         _need(budget >= 1, "budget: 1 or more")
         shape, dev = (B, h, budget), self._index
         if kept is None:
-            kept = torch.empty(shape, dtype=torch.int32, device=self.device)
+            kept = self._kv_new(torch.empty, shape, torch.int32, stream)
         if weights_out is None:
-            weights_out = torch.zeros(shape, dtype=torch.float32, device=self.device)
+            weights_out = self._kv_new(torch.zeros, shape, torch.float32, stream)
         if new_lengths is None:
-            new_lengths = torch.empty((B,), dtype=torch.int32, device=self.device)
+            new_lengths = self._kv_new(torch.empty, (B,), torch.int32, stream)
         _need(kept.dtype is torch.int32 and kept.shape == shape and kept.is_contiguous() and kept.get_device() == dev,
               "kept: int32 [batch, kv_heads, budget]")
         _need(weights_out.dtype is torch.float32 and weights_out.shape == shape and weights_out.is_contiguous() and
@@ -632,14 +636,14 @@ class Context:
         if k_out is None and v_out is None:
             torch = self._torch
             rows = page_table.shape[1] * cache.block if rows is None else rows
-            k_out = torch.zeros((page_table.shape[0], rows, cache.kv_heads, cache.head_dim), dtype=dtype or torch.bfloat16,
-                                device=self.device)
-            v_out = torch.zeros_like(k_out)
+            made = (page_table.shape[0], rows, cache.kv_heads, cache.head_dim)
+            k_out, v_out = (self._kv_new(torch.zeros, made, dtype or torch.bfloat16, stream) for _ in range(2))
         o = k_out if k_out is not None else v_out
         dt = self._kv_dtype(o)
         shape, strides = o.shape, o.stride()
         B = self._kv_seqs(cache, page_table, counts)
-        _need(shape[0] == B and shape[2] == cache.kv_heads and shape[3] == cache.head_dim and _apart(strides, shape),
+        _need(shape[0] == B and shape[2] == cache.kv_heads and shape[3] == cache.head_dim and
+              (o.is_contiguous() or _apart(strides, shape)),
               "outputs: [batch, rows, kv_heads, head_dim], no two elements at one place")
         if k_out is not None and v_out is not None:
             _need(v_out.dtype is o.dtype and v_out.shape == shape and v_out.stride() == strides and

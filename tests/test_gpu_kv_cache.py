@@ -699,6 +699,31 @@ def test_two_streams_at_once(ctx):
         assert torch.equal(out, want) and torch.equal(got, w)
 
 
+def test_results_made_by_the_call_on_another_stream(ctx):
+    """Outputs and workspaces that the call makes itself belong to the stream it was given."""
+    rng = np.random.default_rng(16)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [900], 2, 64, 32, "int8", "bf16")
+    q = normals(rng, (1, 60, 4, 64), "bf16").to(ctx.device)
+    w = torch.rand((1, 2, 900), device=ctx.device)
+    to = torch.tensor([sorted(set(range(cache.pages)) - set(table[0, :29].tolist()))[:1]], dtype=torch.int32, device=ctx.device)
+    s = torch.cuda.Stream()
+
+    def calls(stream):
+        out = ctx.kv_cache_attention(cache, q, dtable, dlen, stream=stream)
+        kept, n, kw = ctx.kv_cache_evict(cache, w, dtable, dlen, 30, 1, 2, dst_table=to, stream=stream)
+        return [out, kept, n, kw, *ctx.kv_cache_read(cache, to, n, rows=32, stream=stream)]
+
+    want = [t.clone() for t in calls(None)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        busy = torch.randn((4096, 4096), device=ctx.device) @ torch.randn((4096, 4096), device=ctx.device)
+        got = calls(s)
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del busy, got
+    ctx.check()
+
+
 def test_refusals(ctx):
     import paper_2601_12150_b200 as spv
     rng = np.random.default_rng(15)
