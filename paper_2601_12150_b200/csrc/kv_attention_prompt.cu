@@ -658,7 +658,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   if (warp == 8) tmem_dealloc(tmem, 512);
 }
 
-// ---- units that were cut: grid (CTA, 256 / kJoinRows) ---------------------------------------------------
+// ---- units that were cut: grid (CTA, parts of the rows) ---------------------------------------------------
 template <int D>
 __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const PromptArgs s, int ctas) {
   constexpr int kLanes = D / 4, kJoinRows = 256 / kLanes;        // a thread has four values of a row
@@ -668,51 +668,56 @@ __global__ void __launch_bounds__(256) kv_prompt_join(const KvView c, const Prom
   const int c0 = share.owner(d.line), c1 = share.owner(d.line + d.tiles - 1), rows = d.n * s.a.group;
   if (c0 != (int)blockIdx.x || c0 == c1) return;
   const int pair = d.b * c.kv_heads + d.head;
-  const int in = blockIdx.y * kJoinRows + threadIdx.x / kLanes, row = d.unit * kRowsUnit + in, col = threadIdx.x % kLanes * 4;
-  float top = -INFINITY, den = 0.0f;
-  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  // four pieces at a time: their loads do not wait for one another
-  for (int i0 = c0; i0 <= c1; i0 += 4) {
-    float2 ml[4];
-    float4 v[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      ml[x] = make_float2(-INFINITY, 0.0f);
-      if (i0 + x <= c1) {
-        const size_t slot = (size_t)(2 * (i0 + x) + (i0 + x == c0)) * kRowsUnit + in;
-        ml[x] = s.part_ml[slot];
-        v[x] = *reinterpret_cast<const float4*>(s.part_o + slot * D + col);
+  const int col = threadIdx.x % kLanes * 4;
+  const float unit = s.refs[pair].y;
+  // a few rows a thread: what it takes to find them costs as much as one
+  for (int in = blockIdx.y * kJoinRows + threadIdx.x / kLanes; in < kRowsUnit; in += gridDim.y * kJoinRows) {
+    const int row = d.unit * kRowsUnit + in;
+    float top = -INFINITY, den = 0.0f;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    // four pieces at a time: their loads do not wait for one another
+    for (int i0 = c0; i0 <= c1; i0 += 4) {
+      float2 ml[4];
+      float4 v[4];
+  #pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        ml[x] = make_float2(-INFINITY, 0.0f);
+        if (i0 + x <= c1) {
+          const size_t slot = (size_t)(2 * (i0 + x) + (i0 + x == c0)) * kRowsUnit + in;
+          ml[x] = s.part_ml[slot];
+          v[x] = *reinterpret_cast<const float4*>(s.part_o + slot * D + col);
+        }
       }
-    }
-    const float next = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
-    const float ref = next == -INFINITY ? 0.0f : next, old = exp2_fast(top - ref);
-    den *= old;
-    sum = make_float4(sum.x * old, sum.y * old, sum.z * old, sum.w * old);
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      if (ml[x].y > 0.0f || ml[x].y != ml[x].y) {          // without a key nothing was written
-        const float f = exp2_fast(ml[x].x - ref);
-        den = fmaf(ml[x].y, f, den);
-        sum.x = fmaf(v[x].x, f, sum.x);
-        sum.y = fmaf(v[x].y, f, sum.y);
-        sum.z = fmaf(v[x].z, f, sum.z);
-        sum.w = fmaf(v[x].w, f, sum.w);
+      const float next = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+      const float ref = next == -INFINITY ? 0.0f : next, old = exp2_fast(top - ref);
+      den *= old;
+      sum = make_float4(sum.x * old, sum.y * old, sum.z * old, sum.w * old);
+  #pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        if (ml[x].y > 0.0f || ml[x].y != ml[x].y) {          // without a key nothing was written
+          const float f = exp2_fast(ml[x].x - ref);
+          den = fmaf(ml[x].y, f, den);
+          sum.x = fmaf(v[x].x, f, sum.x);
+          sum.y = fmaf(v[x].y, f, sum.y);
+          sum.z = fmaf(v[x].z, f, sum.z);
+          sum.w = fmaf(v[x].w, f, sum.w);
+        }
       }
+      top = next;
     }
-    top = next;
+    const bool some = den > 0.0f || den != den, real = row < rows;
+    if (real) {
+      const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
+      const float inv = some ? unit / den : 0.0f;
+      uint2 u;
+      if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv));
+      else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv));
+      *reinterpret_cast<uint2*>(s.a.o + (s.b0 + d.b) * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + col) = u;
+      if (col == 0 && s.a.lse)
+        s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
+    }
+    if (col == 0) s.row_stat[(size_t)pair * s.rows_pad + row] = real && some ? -(top + log2f(den)) : -INFINITY;
   }
-  const bool some = den > 0.0f || den != den, real = row < rows;
-  if (real) {
-    const int i = row / s.a.group, h = d.head * s.a.group + row % s.a.group;
-    const float inv = some ? s.refs[pair].y / den : 0.0f;
-    uint2 u;
-    if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_BF16>(sum.z * inv, sum.w * inv));
-    else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * inv, sum.y * inv), kv_pack2<SPV_FP16>(sum.z * inv, sum.w * inv));
-    *reinterpret_cast<uint2*>(s.a.o + (s.b0 + d.b) * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + col) = u;
-    if (col == 0 && s.a.lse)
-      s.a.lse[((size_t)(s.b0 + d.b) * s.a.tokens + i) * s.a.heads + h] = some ? (top + log2f(den)) * 0.6931471805599453f : -INFINITY;
-  }
-  if (col == 0) s.row_stat[(size_t)pair * s.rows_pad + row] = real && some ? -(top + log2f(den)) : -INFINITY;
 }
 
 // ---- weights: two CTAs an SM, equal stretches of the line of (key tile, row tile) -----------------------
@@ -1107,7 +1112,7 @@ int32_t run(spv_ctx* ctx, const spv_kv_seqs* seqs, const KvView& view, const KvA
     s.nb = seqs->batch - b0 < w.round ? seqs->batch - b0 : w.round;
     kv_prompt_prepare<FMT, D><<<dim3(key_chunks + row_chunks + 1, view.kv_heads, s.nb), kPrepThreads, 0, stream>>>(view, s, key_chunks);
     kv_prompt_attend<D><<<ctas, kAttendThreads, attend_bytes, stream>>>(mq, mk, mv, view, s);
-    kv_prompt_join<D><<<dim3(ctas, kRowsUnit * D / 1024), 256, 0, stream>>>(view, s, ctas);
+    kv_prompt_join<D><<<dim3(ctas, 8), 256, 0, stream>>>(view, s, ctas);
     launches += 3;
     if (a.w_out) {
       kv_prompt_weigh<D><<<2 * ctas, kWeighThreads, weigh_bytes, stream>>>(mq, mk, view, s);
