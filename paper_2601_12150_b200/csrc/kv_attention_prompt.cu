@@ -111,7 +111,7 @@ struct Share {
 
 // One block: all units of the round in order, and where every CTA's stretch begins and ends.  A warp per sequence.
 __device__ void make_plan(const KvView& c, const PromptArgs& s) {
-  __shared__ int seq_units[kPrepThreads], seq_tiles[kPrepThreads], seq_weigh[kPrepThreads];   // of 256 sequences
+  __shared__ int seq_units[kPrepThreads], seq_tiles[kPrepThreads], seq_weigh[kPrepThreads], seq_head[kPrepThreads];   // of 256 sequences
   __shared__ int base_units, base_tiles, base_weigh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) base_units = base_tiles = base_weigh = 0;
@@ -122,24 +122,21 @@ __device__ void make_plan(const KvView& c, const PromptArgs& s) {
       for (int i = warp; i < count; i += kPrepThreads / 32) {
         const int b = b0 + i, len = seq_len(c, s.b0 + b), n = seq_queries(s.a, s.b0 + b);
         const int units = (n * s.a.group + kRowsUnit - 1) / kRowsUnit;
-        const int first = pass ? seq_units[i] : 0, line0 = pass ? seq_tiles[i] : 0;
-        int per_head = 0;
-        for (int h = 0; h < (pass ? c.kv_heads : 1); ++h) {
-          int at = 0;
-          for (int u0 = 0; u0 < units; u0 += 32) {
-            const int u = u0 + lane;
-            const int t = u < units ? block_tiles(len, n, s.a.group, s.a.causal, u * kRowsUnit, (u + 1) * kRowsUnit) : 0;
-            int inc = t;
+        const int first = pass ? seq_units[i] : 0, line0 = pass ? seq_tiles[i] : 0, per_head = pass ? seq_head[i] : 0;
+        int at = 0;                          // tiles of one key head; all have the same
+        for (int u0 = 0; u0 < units; u0 += 32) {
+          const int u = u0 + lane;
+          const int t = u < units ? block_tiles(len, n, s.a.group, s.a.causal, u * kRowsUnit, (u + 1) * kRowsUnit) : 0;
+          int inc = t;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-              const int x = __shfl_up_sync(0xffffffffu, inc, o);
-              if (lane >= o) inc += x;
-            }
-            if (pass && u < units)
-              s.units[first + h * units + u] = Unit{b, h, u, line0 + h * per_head + at + inc - t, t, len, n, 0};
-            at += __shfl_sync(0xffffffffu, inc, 31);
+          for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += x;
           }
-          per_head = at;
+          if (pass && u < units)
+            for (int h = 0; h < c.kv_heads; ++h)
+              s.units[first + h * units + u] = Unit{b, h, u, line0 + h * per_head + at + inc - t, t, len, n, 0};
+          at += __shfl_sync(0xffffffffu, inc, 31);
         }
         if (!pass) {
           int weigh = 0;
@@ -149,7 +146,8 @@ __device__ void make_plan(const KvView& c, const PromptArgs& s) {
           weigh = __reduce_add_sync(0xffffffffu, weigh);
           if (lane == 0) {
             seq_units[i] = units * c.kv_heads;
-            seq_tiles[i] = per_head * c.kv_heads;
+            seq_tiles[i] = at * c.kv_heads;
+            seq_head[i] = at;
             seq_weigh[i] = weigh * c.kv_heads;
           }
         }

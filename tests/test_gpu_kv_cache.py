@@ -320,6 +320,40 @@ def test_attention_long_prompts(ctx, fmt, dtype, dim, group, causal):
                   causal)
 
 
+@pytest.mark.parametrize("heads,tokens", [(40, 1), (128, 1), (33, 3)])
+def test_attention_many_heads_on_one_key_head(ctx, heads, tokens):
+    rng = np.random.default_rng(heads)
+    run_attention(ctx, rng, [500, 0, 70, 129], tokens, None, heads, 1, 128, 64, "int8", "bf16", True)
+
+
+@pytest.mark.parametrize("tokens", [1, 36])
+def test_attention_many_short_sequences(ctx, tokens):
+    """More sequences than a CTA has threads, most of them empty or of a few slots, some without queries."""
+    rng = np.random.default_rng(tokens)
+    lengths = [int(x) for x in rng.integers(0, 40, 700)]
+    lengths[::3] = [0] * len(lengths[::3])
+    lengths[5], lengths[600] = 300, 777
+    counts = [int(rng.integers(0, tokens + 1)) for _ in lengths]
+    run_attention(ctx, rng, lengths, tokens, counts, 2, 1, 64, 16, "e4m3", "bf16", True)
+
+
+@pytest.mark.parametrize("tokens", [1, 7, 90])
+def test_attention_queries_of_all_magnitudes(ctx, tokens):
+    """Neighbouring queries that differ by up to 2^20, and rows of zeros."""
+    rng = np.random.default_rng(23)
+    lengths, heads, kv, dim = [600, 200], 6, 2, 64
+    cache, pool, table, dtable, dlen = filled(ctx, rng, lengths, kv, dim, 32, "int8", "bf16")
+    q = normals(rng, (2, tokens, heads, dim), "bf16")
+    power = torch.from_numpy(rng.integers(-16, 5, (2, tokens, heads, 1)).astype(np.float32))
+    q = (q.float() * torch.exp2(power)).to(torch.bfloat16)
+    q[:, :, 1] = 0
+    got = ctx.kv_cache_attention(cache, q.to(ctx.device), dtable, dlen).cpu().double().numpy()
+    ctx.check()
+    for b, n in enumerate(lengths):
+        o, _, _, spread, reach, vmax = ref.attention(pool, table[b], q[b].double().numpy(), n, tokens, heads, kv, True, 0.125)
+        assert np.all(np.abs(got[b] - o) <= bounds(o, spread, reach, vmax, dim, n, "bf16"))
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_attention_uneven_scales(ctx, fmt):
     """Blocks whose keys and values differ by many powers of two, an all-zero block, one far larger than the rest."""
