@@ -15,6 +15,9 @@
 //   kv_finish_kernel  joins the pieces of pairs that were cut between warps, and turns the stored scores into attention
 //                     weights; its blocks take equal stretches of the same line.
 //
+// Few or short pairs take one launch with a CTA for each (ALONE below): the warps share the tiles of the pair and their
+// results meet in shared memory.
+//
 // Numbers: queries are scaled by a power of two of their own (largest magnitude in [2^14, 2^15)) into fp16, exactly but
 // for elements below 2^-28 of their row's largest; codes are exact in fp16; sums are fp32.  Probabilities are rounded to
 // fp16 for the product with V (relative 2^-11, less than the rounding of the result to bf16) and relative to a maximum
@@ -238,7 +241,55 @@ __device__ __forceinline__ int load_queries(const StreamArgs& s, const Piece& p,
   return ex - 14;
 }
 
-template <int FMT, int D, int NT>
+// Weights of the slots [key0, key1) of a pair from the stored scores, by `threads` threads, of which this is `thread`.  stat:
+// maximum and 1 / sum of every row, and (0, 0) behind an odd last one.
+template <int TILE>
+__device__ __forceinline__ void write_weights(const StreamArgs& s, const Piece& p, const float2* stat, int key0, int key1,
+                                              int thread, int threads) {
+  constexpr int kTile = TILE;
+  const int rows = p.n * s.a.group;
+  const int64_t wat = p.b * s.a.w_stride_b + p.head * s.a.w_stride_head;
+  const float* w_in = s.a.w_in ? s.a.w_in + wat : nullptr;
+  float* w_out = s.a.w_out + wat;
+  const bool wide = (((uintptr_t)w_out | (uintptr_t)w_in) & 15u) == 0;
+  // four keys a thread: the scores of a row are side by side
+  for (int key = key0 + thread * 4; key < key1; key += threads * 4) {
+    const float* zt = s.z + (size_t)(p.line + key / kTile) * s.rows * kTile + key % kTile * 2;
+    const bool four = wide && key + 4 <= key1;
+    float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (w_in) {
+      if (four) {
+        w = *reinterpret_cast<const float4*>(w_in + key);
+      } else {
+        w.x = w_in[key];
+        if (key + 1 < key1) w.y = w_in[key + 1];
+        if (key + 2 < key1) w.z = w_in[key + 2];
+        if (key + 3 < key1) w.w = w_in[key + 3];
+      }
+    }
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 2
+    for (int row = 0; row < rows; row += 2) {
+      const float4 u = *reinterpret_cast<const float4*>(zt + row * kTile), v = *reinterpret_cast<const float4*>(zt + row * kTile + 4);
+      const float2 s0 = stat[row], s1 = stat[row + 1];
+      sum.x = fmaf(exp2_fast(u.x - s0.x), s0.y, fmaf(exp2_fast(u.y - s1.x), s1.y, sum.x));
+      sum.y = fmaf(exp2_fast(u.z - s0.x), s0.y, fmaf(exp2_fast(u.w - s1.x), s1.y, sum.y));
+      sum.z = fmaf(exp2_fast(v.x - s0.x), s0.y, fmaf(exp2_fast(v.y - s1.x), s1.y, sum.z));
+      sum.w = fmaf(exp2_fast(v.z - s0.x), s0.y, fmaf(exp2_fast(v.w - s1.x), s1.y, sum.w));
+    }
+    w = make_float4(w.x + sum.x, w.y + sum.y, w.z + sum.z, w.w + sum.w);
+    if (four) {
+      *reinterpret_cast<float4*>(w_out + key) = w;
+    } else {
+      w_out[key] = w.x;
+      if (key + 1 < key1) w_out[key + 1] = w.y;
+      if (key + 2 < key1) w_out[key + 2] = w.z;
+      if (key + 3 < key1) w_out[key + 3] = w.w;
+    }
+  }
+}
+
+template <int FMT, int D, int NT, bool ALONE>
 __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
     kv_stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const KvView c,
                      const StreamArgs s) {
@@ -272,24 +323,41 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
       if (s.a.counts) kv_clamped(__ldg(s.a.counts + b), s.a.tokens, c.status);
     }
   }
-  // neighbours on the line are on different SMs, so that few tiles are spread over all of them
-  const int workers = gridDim.x * kWarps, worker = warp * gridDim.x + blockIdx.x;
-  scan_tiles<L::kThreads, kTile>(c, s.a, scan, [&](int total, int w) {
-    const Share share(total, workers);
-    const int at = w * gridDim.x + blockIdx.x;
-    return at < share.working ? share.begin(at) : total;
-  });
-  const Share share(scan->total, workers);
-  Walk walk;
-  walk.before = scan->before[warp];
-  walk.b = scan->b[warp];
-  if (worker >= share.working) {
-    if (lane == 0) s.stretch[worker].total = scan->total;
-    return;
+  Piece p{};
+  Walk walk{};
+  int workers = 0, worker = 0, stretch;
+  constexpr int kStep = ALONE ? kWarps : 1;              // from one tile of a warp to its next
+  if constexpr (ALONE) {
+    // one pair a CTA, its tiles for the warps in turn
+    p.b = blockIdx.x / c.kv_heads;
+    p.head = blockIdx.x % c.kv_heads;
+    p.len = seq_len(c, p.b);
+    p.n = seq_queries(s.a, p.b);
+    p.tiles = p.kt1 = p.n > 0 ? (p.len + kTile - 1) / kTile : 0;
+    p.kt0 = warp;
+    p.line = blockIdx.x * ((c.max_length + kTile - 1) / kTile);
+    stretch = p.tiles > warp ? (p.tiles - warp + kWarps - 1) / kWarps : 0;
+    __syncthreads();                                     // the barriers are there
+  } else {
+    // neighbours on the line are on different SMs, so that few tiles are spread over all of them
+    workers = gridDim.x * kWarps;
+    worker = warp * gridDim.x + blockIdx.x;
+    scan_tiles<L::kThreads, kTile>(c, s.a, scan, [&](int total, int w) {
+      const Share share(total, workers);
+      const int at = w * gridDim.x + blockIdx.x;
+      return at < share.working ? share.begin(at) : total;
+    });
+    const Share share(scan->total, workers);
+    walk.before = scan->before[warp];
+    walk.b = scan->b[warp];
+    if (worker >= share.working) {
+      if (lane == 0) s.stretch[worker].total = scan->total;
+      return;
+    }
+    walk.pos = share.begin(worker);
+    walk.end = share.begin(worker + 1);
+    stretch = walk.end - walk.pos;
   }
-  walk.pos = share.begin(worker);
-  walk.end = share.begin(worker + 1);
-  Piece p;
 
   // ---- what this warp brings in: tiles of its stretch, kOwn ahead of the one it works on
   uint64_t policy;
@@ -298,10 +366,9 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
   const int lparts = 31 - __clz(kTile / part);         // a tile has 2^lparts copies: 1, 2 or 4
   const int parts = 1 << lparts;
   const int lblock = 31 - __clz(s.a.block);
-  const int stretch = walk.end - walk.pos;
   Walk fwalk = walk;
-  Piece fp;
-  int f_begin = 0, f_end = 0, f_batch = -1;            // tiles of the piece being fed; first tile of the lanes' batch
+  Piece fp = p;
+  int f_begin = 0, f_end = ALONE ? stretch : 0, f_batch = -1;            // tiles of the piece being fed; first tile of the lanes' batch
   int f_row = -1, f_lost = 0;                          // this lane's copy: line of the pool, or none
   float f_ks = 0.0f, f_vs = 0.0f;
   // tile `it` of the stretch into stage `st`; the lanes know the pages of the next 32 / parts tiles
@@ -317,7 +384,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
     if (at >= 32) {
       f_batch = it;
       at = 0;
-      const int mine = it + (lane >> lparts), slot = (fp.kt0 + mine - f_begin) * kTile + (lane & (parts - 1)) * part;
+      const int mine = it + (lane >> lparts), slot = (fp.kt0 + (mine - f_begin) * kStep) * kTile + (lane & (parts - 1)) * part;
       f_row = -1;
       f_lost = 0;
       f_ks = f_vs = 0.0f;                              // of parts that hold nothing
@@ -371,8 +438,8 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
 
   const int r = lane >> 2, q2 = (lane & 3) * 2;
   int it = 0;                  // tile of the stretch
-  while (next_piece<kTile>(c, s.a, walk, p)) {
-    if (it == 0 && lane == 0) s.stretch[worker] = Stretch{scan->total, walk.before, p.b, p.head, p.len, p.n, p.tiles, p.kt0};
+  for (bool first = true; ALONE ? first : next_piece<kTile>(c, s.a, walk, p); first = false) {
+    if (!ALONE && it == 0 && lane == 0) s.stretch[worker] = Stretch{scan->total, walk.before, p.b, p.head, p.len, p.n, p.tiles, p.kt0};
     const int full_end = spv_kv_query_end(p.len, p.n, 0, s.a.causal);     // slots that every query sees (the first sees least)
     float o[kSteps][NT][4];
     float m[NT][2], l[NT][2], qf[NT][2];
@@ -399,7 +466,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[j][t][e] = 0.0f;
     }
-    for (int kt = p.kt0; kt < p.kt1; ++kt, ++it) {
+    for (int kt = p.kt0; kt < p.kt1; kt += kStep, ++it) {
       const int st = own + slot_at;
       mbar_wait(full + st, phase, abort_flag, wait_status, 0x4B02u);
       const uint32_t kbase = smem_u32(smem) + st * L::kStageBytes, vbase = kbase + kTile * D;
@@ -601,6 +668,71 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
       }
     }
 
+    if constexpr (ALONE) {
+      // ---- the warps' results meet: each leaves its own, relative to its own maxima, in its stages
+      __syncwarp();            // its queries and stages are read no more
+      float* mine = reinterpret_cast<float*>(smem + own * L::kStageBytes);
+      static_assert(kRows * D * 4 + (NT == 4 ? 0 : kRows * 8) <= L::kOwn * L::kStageBytes, "a warp's results fit its stages");
+      static_assert(kRows * 8 <= 256, "the rows' sums stand before the abort flag");
+      auto ml_of = [&](int w) {
+        return reinterpret_cast<float2*>(NT == 4 ? smem + L::oQ + w * (L::kQ / kWarps)
+                                                 : smem + w * L::kOwn * L::kStageBytes + kRows * D * 4);
+      };
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int sh = 4; sh < 32; sh <<= 1) l[t][e] += __shfl_xor_sync(0xffffffffu, l[t][e], sh);
+          const int row = 8 * t + q2 + e;
+          float* at = mine + row * D + r * (D / 8);
+#pragma unroll
+          for (int j = 0; j < kSteps; j += 2)
+            *reinterpret_cast<float4*>(at + 2 * j) = make_float4(o[j][t][e] * vref, o[j][t][e + 2] * vref,
+                                                                 o[j + 1][t][e] * vref, o[j + 1][t][e + 2] * vref);
+          if (r == 0) ml_of(warp)[row] = make_float2(m[t][e], l[t][e]);
+        }
+      __syncthreads();
+      const int rows = p.n * s.a.group;
+      float2* stat = reinterpret_cast<float2*>(scan);    // maximum, 1 / sum of a row
+      if ((int)threadIdx.x < kRows) {
+        float top = -INFINITY, den = 0.0f;
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml_of(w)[threadIdx.x].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        for (int w = 0; w < kWarps; ++w) {
+          const float2 ml = ml_of(w)[threadIdx.x];
+          den += ml.y * exp2_fast(ml.x - ref);
+        }
+        const bool real = (int)threadIdx.x < rows;
+        stat[threadIdx.x] = real ? make_float2(ref, den == 0.0f ? 0.0f : 1.0f / den) : make_float2(0.0f, 0.0f);
+        if (real && s.a.lse) {
+          const int i = threadIdx.x / s.a.group, h = p.head * s.a.group + threadIdx.x % s.a.group;
+          s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + h] = den == 0.0f ? -INFINITY : (top + log2f(den)) * 0.6931471805599453f;
+        }
+      }
+      __syncthreads();
+      for (int x = threadIdx.x; x < rows * (D / 4); x += L::kThreads) {
+        const int row = x / (D / 4), d = x % (D / 4) * 4;
+        const float2 st = stat[row];
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 v = *reinterpret_cast<const float4*>(smem + w * L::kOwn * L::kStageBytes + (row * D + d) * 4);
+          const float f = exp2_fast(ml_of(w)[row].x - st.x) * st.y;
+          sum.x = fmaf(v.x, f, sum.x);
+          sum.y = fmaf(v.y, f, sum.y);
+          sum.z = fmaf(v.z, f, sum.z);
+          sum.w = fmaf(v.w, f, sum.w);
+        }
+        const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
+        uint2 u;
+        if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x, sum.y), kv_pack2<SPV_BF16>(sum.z, sum.w));
+        else u = make_uint2(kv_pack2<SPV_FP16>(sum.x, sum.y), kv_pack2<SPV_FP16>(sum.z, sum.w));
+        *reinterpret_cast<uint2*>(s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + d) = u;
+      }
+      if (s.a.w_out) write_weights<kTile>(s, p, stat, 0, p.len, threadIdx.x, L::kThreads);
+      continue;
+    }
     // ---- results of the piece: the pair's, or a part of them
     const bool whole = p.kt0 == 0 && p.kt1 == p.tiles;
     const int which = p.kt0 > 0 ? 0 : 1;
@@ -785,46 +917,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
       }
       continue;
     }
-    const int64_t wat = p.b * s.a.w_stride_b + p.head * s.a.w_stride_head;
-    const int key1 = min(p.len, p.kt1 * kTile);
-    const float* w_in = s.a.w_in ? s.a.w_in + wat : nullptr;
-    float* w_out = s.a.w_out + wat;
-    const bool wide = (((uintptr_t)w_out | (uintptr_t)w_in) & 15u) == 0;
-    // four keys a thread: the scores of a row are side by side
-    for (int key = p.kt0 * kTile + ((int)threadIdx.x - joiners) * 4; key < key1; key += joiners * 4) {
-      const float* zt = s.z + (size_t)(p.line + key / kTile) * s.rows * kTile + key % kTile * 2;
-      const bool four = wide && key + 4 <= key1;
-      float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (w_in) {
-        if (four) {
-          w = *reinterpret_cast<const float4*>(w_in + key);
-        } else {
-          w.x = w_in[key];
-          if (key + 1 < key1) w.y = w_in[key + 1];
-          if (key + 2 < key1) w.z = w_in[key + 2];
-          if (key + 3 < key1) w.w = w_in[key + 3];
-        }
-      }
-      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 2
-      for (int row = 0; row < rows; row += 2) {
-        const float4 u = *reinterpret_cast<const float4*>(zt + row * kTile), v = *reinterpret_cast<const float4*>(zt + row * kTile + 4);
-        const float2 s0 = stat[row], s1 = stat[row + 1];
-        sum.x = fmaf(exp2_fast(u.x - s0.x), s0.y, fmaf(exp2_fast(u.y - s1.x), s1.y, sum.x));
-        sum.y = fmaf(exp2_fast(u.z - s0.x), s0.y, fmaf(exp2_fast(u.w - s1.x), s1.y, sum.y));
-        sum.z = fmaf(exp2_fast(v.x - s0.x), s0.y, fmaf(exp2_fast(v.y - s1.x), s1.y, sum.z));
-        sum.w = fmaf(exp2_fast(v.z - s0.x), s0.y, fmaf(exp2_fast(v.w - s1.x), s1.y, sum.w));
-      }
-      w = make_float4(w.x + sum.x, w.y + sum.y, w.z + sum.z, w.w + sum.w);
-      if (four) {
-        *reinterpret_cast<float4*>(w_out + key) = w;
-      } else {
-        w_out[key] = w.x;
-        if (key + 1 < key1) w_out[key + 1] = w.y;
-        if (key + 2 < key1) w_out[key + 2] = w.z;
-        if (key + 3 < key1) w_out[key + 3] = w.w;
-      }
-    }
+    write_weights<kTile>(s, p, stat, p.kt0 * kTile, min(p.len, p.kt1 * kTile), (int)threadIdx.x - joiners, joiners);
   }
 }
 
@@ -849,13 +942,13 @@ Workspace plan(const spv_kv_cache* c, const spv_kv_seqs* q, const spv_kv_attn_de
   return w;
 }
 
-template <int FMT, int D, int NT>
+template <int FMT, int D, int NT, bool ALONE>
 int32_t launch(spv_ctx* ctx, int which, const CUtensorMap& mk, const CUtensorMap& mv, const KvView& view, const StreamArgs& s,
                int ctas, cudaStream_t stream) {
   constexpr int bytes = Layout<D, NT>::kTotal + 1024;
   static_assert(bytes <= 227 * 1024, "shared memory");
   static_assert(Layout<D, NT>::kOwn >= 2, "a warp works on one stage while another fills");
-  auto kernel = kv_stream_kernel<FMT, D, NT>;
+  auto kernel = kv_stream_kernel<FMT, D, NT, ALONE>;
   if (!(ctx->kv_configured & (1u << which))) {
     SPV_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     ctx->kv_configured |= 1u << which;
@@ -899,13 +992,28 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if ((st = spv_make_tmap_u8(ctx, &mv, cache->v, 2, dims, strides, box)) != SPV_OK) return st;
   const int64_t most = (int64_t)seqs->batch * cache->kv_heads * ((view.max_length + tile - 1) / tile);
   int ctas = ctx->sm_count < kMaxSms ? ctx->sm_count : kMaxSms;
-  if (most < ctas) ctas = (int)most;
   const int slots = row_slots_of(s.rows);
+  // One pair a CTA, or the line and its second kernel?  A wave of CTAs costs the tiles of a warp and about two more; the
+  // line costs its tiles, each about twice (the finishing kernel), and a fixed five.  Measured in us, alone against the line,
+  // equal lengths: 16 pairs of 785 slots of 64: 8.5, 12.9; 128 of 1536: 10.0, 19.4; 128 of 3000 slots of 128: 23, 35; 512 of
+  // 380: 25, 34; but 8 pairs of 2200: 17.5, 15.1; 512 of 100: 22, 20; 4096 of 50 slots of 64: 146, 40.  The bound of twelve
+  // keeps one long pair among short ones from holding up the call.
+  const int64_t pairs = (int64_t)seqs->batch * cache->kv_heads;
+  const int64_t waves = (pairs + ctas - 1) / ctas, warps = warps_of(slots);
+  const int64_t alone_cost = waves * (((view.max_length + tile - 1) / tile + warps - 1) / warps + 2);
+  const int64_t line_cost = 5 + 2 * ((most + ctas * warps - 1) / (ctas * warps));
+  const bool alone = alone_cost <= line_cost && alone_cost <= 12;
+  if (!alone && most < ctas) ctas = (int)most;
   auto go = [&](auto fmt, auto dim) -> int32_t {
-    constexpr int base_id = (fmt() * 2 + (dim() == 128)) * 3;
-    if (slots == 8) return launch<fmt(), dim(), 1>(ctx, base_id, mk, mv, view, s, ctas, stream);
-    if (slots == 16) return launch<fmt(), dim(), 2>(ctx, base_id + 1, mk, mv, view, s, ctas, stream);
-    return launch<fmt(), dim(), 4>(ctx, base_id + 2, mk, mv, view, s, ctas, stream);
+    constexpr int id = (fmt() * 2 + (dim() == 128)) * 6;
+    if (alone) {
+      if (slots == 8) return launch<fmt(), dim(), 1, true>(ctx, id + 3, mk, mv, view, s, (int)pairs, stream);
+      if (slots == 16) return launch<fmt(), dim(), 2, true>(ctx, id + 4, mk, mv, view, s, (int)pairs, stream);
+      return launch<fmt(), dim(), 4, true>(ctx, id + 5, mk, mv, view, s, (int)pairs, stream);
+    }
+    if (slots == 8) return launch<fmt(), dim(), 1, false>(ctx, id, mk, mv, view, s, ctas, stream);
+    if (slots == 16) return launch<fmt(), dim(), 2, false>(ctx, id + 1, mk, mv, view, s, ctas, stream);
+    return launch<fmt(), dim(), 4, false>(ctx, id + 2, mk, mv, view, s, ctas, stream);
   };
   using I8 = std::integral_constant<int, SPV_KV_INT8>;
   using E4 = std::integral_constant<int, SPV_KV_E4M3>;
@@ -914,10 +1022,11 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   if (cache->format == SPV_KV_INT8) st = cache->head_dim == 64 ? go(I8(), D64()) : go(I8(), D128());
   else st = cache->head_dim == 64 ? go(E4(), D64()) : go(E4(), D128());
   if (st != SPV_OK) return st;
+  if (alone) return spv_launch_ok(ctx, 1);
   const int workers = ctas * warps_of(slots);
   const int64_t used = most < workers ? most : workers;
-  // as many blocks as are resident at once, four an SM; of few workers each has its own (785 slots, 16 heads: 12.7 us for
-  // the step instead of 15 with three to a block)
+  // as many blocks as are resident at once, four an SM; of few workers each has its own (16 pairs of 785 slots, when
+  // lined up: 12.7 us for the step instead of 15 with three to a block)
   const int per_block = (int)((used + 4 * ctas - 1) / (4 * ctas));
   const unsigned blocks = (unsigned)((used + per_block - 1) / per_block);
   if (cache->head_dim == 64) kv_finish_kernel<64><<<blocks, kFinishThreads, 0, stream>>>(view, s, workers, slots, per_block);

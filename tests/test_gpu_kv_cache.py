@@ -337,6 +337,31 @@ def test_attention_many_short_sequences(ctx, tokens):
     run_attention(ctx, rng, lengths, tokens, counts, 2, 1, 64, 16, "e4m3", "bf16", True)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("block,dim,group,tokens", [(16, 64, 1, 1), (64, 128, 5, 1), (128, 64, 4, 4), (32, 128, 9, 3),
+                                                    (128, 128, 31, 1)])
+@pytest.mark.parametrize("room", [0, 4000])
+def test_attention_few_short_pairs(ctx, dtype, block, dim, group, tokens, room):
+    """Short sequences in a table that fits them, and in one with room for far longer: a pair's tiles shared by the warps
+    of one CTA, or lined up with the others'; one to two tiles a warp, none, and rows that see nothing."""
+    rng = np.random.default_rng(block + dim + group)
+    tile = 8192 // (2 * dim)
+    for lengths in ([1], [tile * 12 - 1, tile * 8, 0, 2], [tile * 16 - block, tile * 9 + 1, 5, 0]):
+        counts = [tokens - b % 2 for b in range(len(lengths))]
+        state = filled(ctx, rng, lengths, 2, dim, block, "e4m3", dtype, room=room)
+        run_attention(ctx, rng, lengths, tokens, counts, 2 * group, 2, dim, block, "e4m3", dtype, True, state=state)
+    run_attention(ctx, rng, lengths, tokens, counts, 2 * group, 2, dim, block, "e4m3", dtype, False, weights=False, state=state)
+
+
+@pytest.mark.parametrize("sequences,tiles", [(149, 2), (74, 24), (3, 25), (8, 60), (8, 61), (260, 3), (290, 12), (300, 12),
+                                             (60, 120), (60, 121)])
+def test_attention_where_the_pairs_become_many_or_long(ctx, sequences, tiles):
+    rng = np.random.default_rng(sequences)
+    lengths = [int(x) for x in rng.integers(0, 60, sequences)]
+    lengths[-1] = tiles * 64 - 70                    # the table has a page more than the longest needs
+    run_attention(ctx, rng, lengths, 1, None, 2, 2, 64, 64, "int8", "fp16", True)
+
+
 @pytest.mark.parametrize("tokens", [1, 7, 90])
 def test_attention_queries_of_all_magnitudes(ctx, tokens):
     """Neighbouring queries that differ by up to 2^20, and rows of zeros."""
