@@ -793,28 +793,33 @@ constexpr int kFinishThreads = 256;
 __device__ __forceinline__ const float2* part_ml(const StreamArgs& s, int workers, int row, int worker, int c0) {
   return s.part_ml + (size_t)(2 * row + (worker == c0)) * workers + worker;
 }
-// Maximum and sum of a row over the pieces of a pair, those of workers c0 .. c1; a whole warp.
-__device__ __forceinline__ float2 joined(const StreamArgs& s, int workers, int c0, int c1, int row) {
-  const int lane = threadIdx.x & 31;
-  float top = -INFINITY, den = 0.0f;
-  for (int i = c0 + lane; i <= c1; i += 128) {
-    float2 ml[4];
+// Maximum and sum of `x` over `lanes` neighbouring threads; with it, what the caller's other sums are to be scaled by.
+__device__ __forceinline__ float2 join_lanes(float top, float den, int lanes, float* scale) {
+  float all = top;
+  for (int o = lanes >> 1; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+  *scale = exp2_fast(top - (all == -INFINITY ? 0.0f : all));
+  den *= *scale;
+  for (int o = lanes >> 1; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+  return make_float2(all, den);
+}
+// Maximum and sum of a row over the pieces of a pair, those of workers c0 .. c1, by `lanes` threads, of which this is `sub`.
+__device__ __forceinline__ float2 joined(const StreamArgs& s, int workers, int c0, int c1, int row, int sub, int lanes) {
+  float top = -INFINITY, den = 0.0f, scale;
+  for (int i = c0 + sub; i <= c1; i += 8 * lanes) {
+    float2 ml[8];
+    float m = top;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) ml[x] = i + 32 * x <= c1 ? *part_ml(s, workers, row, i + 32 * x, c0) : make_float2(-INFINITY, 0.0f);
-    const float m = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+    for (int x = 0; x < 8; ++x) {
+      ml[x] = i + x * lanes <= c1 ? *part_ml(s, workers, row, i + x * lanes, c0) : make_float2(-INFINITY, 0.0f);
+      m = fmaxf(m, ml[x].x);
+    }
     const float ref = m == -INFINITY ? 0.0f : m;
     den *= exp2_fast(top - ref);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) den += ml[x].y * exp2_fast(ml[x].x - ref);
+    for (int x = 0; x < 8; ++x) den += ml[x].y * exp2_fast(ml[x].x - ref);
     top = m;
   }
-  float all = top;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-  den *= exp2_fast(top - (all == -INFINITY ? 0.0f : all));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-  return make_float2(all, den);
+  return join_lanes(top, den, lanes, &scale);
 }
 
 // A sequence without a tile: no keys (zeros) or no queries (the weights stay as they are).
@@ -834,13 +839,15 @@ __device__ __forceinline__ void write_empty(const KvView& c, const KvAttnArgs& a
     }
 }
 
-// A block takes the stretches of a few workers; half of its threads joins pieces while the other makes weights.
+__device__ __forceinline__ void weights_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
+
+// A block takes the stretches of a few workers; a quarter of its threads joins pieces while the others make weights (half and
+// half: 1 us more for 262147 slots).
 template <int D>
 __global__ void __launch_bounds__(kFinishThreads, 4)
     kv_finish_kernel(const KvView c, const StreamArgs s, int workers, int row_slots, int per_block) {
   constexpr int kTile = tile_of(D);
-  __shared__ float2 stat[kKvStreamMaxRows + 1]; // maximum, 1 / sum of a row
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float2 stat[kKvStreamMaxRows]; // maximum, 1 / sum of a row
   for (int b = blockIdx.x; b < s.a.batch; b += gridDim.x)
     if (seq_key_tiles<kTile>(c, s.a, b) == 0) write_empty<D>(c, s.a, b);
   const int first = blockIdx.x * per_block;
@@ -854,31 +861,16 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
   w.b = at.b;
   Piece p{at.b, at.head, at.len, at.n, at.tiles, at.kt0, min(at.tiles, at.kt0 + w.end - w.pos), w.pos - at.kt0};
   w.pos += p.kt1 - p.kt0;
-  const int joiners = s.a.w_out ? kFinishThreads / 2 : kFinishThreads;
+  const int joiners = s.a.w_out ? kFinishThreads / 4 : kFinishThreads;
   bool more = true;
   for (; more; more = next_piece<kTile>(c, s.a, w, p)) {
     const int c0 = share.owner(p.line), c1 = share.owner(p.line + p.tiles - 1);
     if (c0 == c1 && !s.a.w_out) continue;
     const int rows = p.n * s.a.group;
-    const size_t pair = (size_t)(p.b * c.kv_heads + p.head) * row_slots;
-    __syncthreads();                            // stat of the piece before is read no more
-    if ((rows & 1) && threadIdx.x == 0) stat[rows] = make_float2(0.0f, 0.0f);       // of the pair's row that there is not
-    for (int row = warp; row < rows; row += kFinishThreads / 32) {
-      const float2 ml = c0 == c1 ? s.pair_ml[pair + row] : joined(s, workers, c0, c1, row);
-      if (lane == 0) {
-        stat[row] = make_float2(ml.x == -INFINITY ? 0.0f : ml.x, ml.y == 0.0f ? 0.0f : 1.0f / ml.y);
-        if (c0 != c1 && p.kt0 == 0 && s.a.lse) {
-          const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
-          s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + h] =
-              ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
-        }
-      }
-    }
-    __syncthreads();
     if ((int)threadIdx.x < joiners) {
       if (c0 == c1) continue;
       // the blocks that meet the pair share its columns (four values of a row), and as many threads as there are share
-      // a column's pieces
+      // a column's pieces; each finds the row's maximum and sum among them by itself, so that nothing waits for them
       const int f0 = c0 / per_block, f1 = c1 / per_block, mine = blockIdx.x - f0;
       const int columns = rows * (D / 4);
       const int x0 = columns * mine / (f1 - f0 + 1), x1 = columns * (mine + 1) / (f1 - f0 + 1);
@@ -887,20 +879,39 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
       for (int xb = x0; xb < x1; xb += joiners / lanes) {
         const int x = xb + (int)threadIdx.x / lanes;
         const int row = x / (D / 4), d = x % (D / 4) * 4;
+        float top = -INFINITY, den = 0.0f, f;
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (x < x1) {
-          const float2 st = stat[row];
-#pragma unroll 4
-          for (int y = c0 + sub; y <= c1; y += lanes) {
-            const float m = part_ml(s, workers, row, y, c0)->x;
-            const float4 v = *reinterpret_cast<const float4*>(s.part_o + ((size_t)(2 * y + (y == c0)) * row_slots + row) * D + d);
-            const float f = exp2_fast(m - st.x) * st.y;
-            sum.x = fmaf(v.x, f, sum.x);
-            sum.y = fmaf(v.y, f, sum.y);
-            sum.z = fmaf(v.z, f, sum.z);
-            sum.w = fmaf(v.w, f, sum.w);
+        for (int i = c0 + sub; x < x1 && i <= c1; i += 4 * lanes) {
+          float2 ml[4];
+          float4 v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int y = i + j * lanes;
+            ml[j] = make_float2(-INFINITY, 0.0f);
+            v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (y <= c1) {
+              ml[j] = *part_ml(s, workers, row, y, c0);
+              v[j] = *reinterpret_cast<const float4*>(s.part_o + ((size_t)(2 * y + (y == c0)) * row_slots + row) * D + d);
+            }
           }
+          const float m = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
+          const float ref = m == -INFINITY ? 0.0f : m;
+          f = exp2_fast(top - ref);
+          den *= f;
+          sum = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f = exp2_fast(ml[j].x - ref);
+            den = fmaf(ml[j].y, f, den);
+            sum.x = fmaf(v[j].x, f, sum.x);
+            sum.y = fmaf(v[j].y, f, sum.y);
+            sum.z = fmaf(v[j].z, f, sum.z);
+            sum.w = fmaf(v[j].w, f, sum.w);
+          }
+          top = m;
         }
+        const float2 ml = join_lanes(top, den, lanes, &f);
+        sum = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
         for (int o = lanes >> 1; o > 0; o >>= 1) {
           sum.x += __shfl_xor_sync(0xffffffffu, sum.x, o);
           sum.y += __shfl_xor_sync(0xffffffffu, sum.y, o);
@@ -909,15 +920,29 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
         }
         if (x < x1 && sub == 0) {
           const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
+          f = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;                   // (a NaN stays one)
           uint2 u;
-          if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x, sum.y), kv_pack2<SPV_BF16>(sum.z, sum.w));
-          else u = make_uint2(kv_pack2<SPV_FP16>(sum.x, sum.y), kv_pack2<SPV_FP16>(sum.z, sum.w));
+          if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * f, sum.y * f), kv_pack2<SPV_BF16>(sum.z * f, sum.w * f));
+          else u = make_uint2(kv_pack2<SPV_FP16>(sum.x * f, sum.y * f), kv_pack2<SPV_FP16>(sum.z * f, sum.w * f));
           *reinterpret_cast<uint2*>(s.a.o + p.b * s.a.o_stride_b + i * s.a.o_stride_tok + h * s.a.o_stride_head + d) = u;
+          if (s.a.lse && d == 0)
+            s.a.lse[((size_t)p.b * s.a.tokens + i) * s.a.heads + h] =
+                ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
         }
       }
       continue;
     }
-    write_weights<kTile>(s, p, stat, p.kt0 * kTile, min(p.len, p.kt1 * kTile), (int)threadIdx.x - joiners, joiners);
+    // ---- weights, by the others
+    const int thread = threadIdx.x - joiners, threads = kFinishThreads - joiners;
+    const int lanes = 128 / row_slots, row = thread / lanes;       // (of the first 128 threads)
+    weights_sync(threads);                     // stat of the piece before is read no more
+    float2 ml = make_float2(-INFINITY, 0.0f);
+    if (c0 != c1) ml = joined(s, workers, c0, row < rows ? c1 : c0 - 1, row, thread & (lanes - 1), lanes);
+    else if (row < rows) ml = s.pair_ml[(size_t)(p.b * c.kv_heads + p.head) * row_slots + row];
+    if (row < row_slots && (thread & (lanes - 1)) == 0)
+      stat[row] = make_float2(ml.x == -INFINITY ? 0.0f : ml.x, row >= rows || ml.y == 0.0f ? 0.0f : 1.0f / ml.y);
+    weights_sync(threads);
+    write_weights<kTile>(s, p, stat, p.kt0 * kTile, min(p.len, p.kt1 * kTile), thread, threads);
   }
 }
 
@@ -994,14 +1019,14 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   int ctas = ctx->sm_count < kMaxSms ? ctx->sm_count : kMaxSms;
   const int slots = row_slots_of(s.rows);
   // One pair a CTA, or the line and its second kernel?  A wave of CTAs costs the tiles of a warp and about two more; the
-  // line costs its tiles, each about twice (the finishing kernel), and a fixed five.  Measured in us, alone against the line,
+  // line costs its tiles, each about twice (the finishing kernel), and a fixed four.  Measured in us, alone against the line,
   // equal lengths: 16 pairs of 785 slots of 64: 8.5, 12.9; 128 of 1536: 10.0, 19.4; 128 of 3000 slots of 128: 23, 35; 512 of
   // 380: 25, 34; but 8 pairs of 2200: 17.5, 15.1; 512 of 100: 22, 20; 4096 of 50 slots of 64: 146, 40.  The bound of twelve
   // keeps one long pair among short ones from holding up the call.
   const int64_t pairs = (int64_t)seqs->batch * cache->kv_heads;
   const int64_t waves = (pairs + ctas - 1) / ctas, warps = warps_of(slots);
   const int64_t alone_cost = waves * (((view.max_length + tile - 1) / tile + warps - 1) / warps + 2);
-  const int64_t line_cost = 5 + 2 * ((most + ctas * warps - 1) / (ctas * warps));
+  const int64_t line_cost = 4 + 2 * ((most + ctas * warps - 1) / (ctas * warps));
   const bool alone = alone_cost <= line_cost && alone_cost <= 12;
   if (!alone && most < ctas) ctas = (int)most;
   auto go = [&](auto fmt, auto dim) -> int32_t {
