@@ -831,12 +831,12 @@ __device__ __forceinline__ void write_empty(const KvView& c, const KvAttnArgs& a
     *reinterpret_cast<uint4*>(a.o + b * a.o_stride_b + i * a.o_stride_tok + h * a.o_stride_head + d) = make_uint4(0u, 0u, 0u, 0u);
     if (a.lse && d == 0) a.lse[((size_t)b * a.tokens + i) * a.heads + h] = -INFINITY;
   }
-  if (!a.w_out || n > 0) return;
-  for (int x = threadIdx.x; x < len; x += blockDim.x)
-    for (int h = 0; h < c.kv_heads; ++h) {
-      const int64_t at = b * a.w_stride_b + h * a.w_stride_head + x;
-      a.w_out[at] = a.w_in ? a.w_in[at] : 0.0f;
-    }
+  if (!a.w_out || n > 0 || a.w_out == a.w_in) return;
+  for (int h = 0; h < c.kv_heads; ++h) {
+    const int64_t at = b * a.w_stride_b + h * a.w_stride_head;
+#pragma unroll 4
+    for (int x = threadIdx.x; x < len; x += blockDim.x) a.w_out[at + x] = a.w_in ? a.w_in[at + x] : 0.0f;
+  }
 }
 
 __device__ __forceinline__ void weights_sync(int threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }

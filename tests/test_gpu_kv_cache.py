@@ -362,6 +362,27 @@ def test_attention_where_the_pairs_become_many_or_long(ctx, sequences, tiles):
     run_attention(ctx, rng, lengths, 1, None, 2, 2, 64, 64, "int8", "fp16", True)
 
 
+@pytest.mark.parametrize("length,room", [(300, 0), (300, 9000), (9000, 0)])
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_attention_weights_of_sequences_that_ask_nothing(ctx, length, room, tokens):
+    """They stay as they are: added up in place, carried over to another tensor, or zeros where there were none."""
+    rng = np.random.default_rng(length + tokens)
+    cache, pool, table, dtable, dlen = filled(ctx, rng, [length, 77, length - 5], 2, 64, 64, "int8", "bf16", room=room)
+    q = normals(rng, (3, tokens, 4, 64), "bf16").to(ctx.device)
+    counts = torch.tensor([0, tokens, 0], dtype=torch.int32, device=ctx.device)
+    before = torch.from_numpy(rng.random((3, 2, length)).astype(np.float32)).to(ctx.device)
+    place, other, fresh = before.clone(), torch.full_like(before, 7.0), torch.full_like(before, 7.0)
+    ctx.kv_cache_attention(cache, q, dtable, dlen, counts=counts, weights_in=place, weights_out=place)
+    ctx.kv_cache_attention(cache, q, dtable, dlen, counts=counts, weights_in=before, weights_out=other)
+    ctx.kv_cache_attention(cache, q, dtable, dlen, counts=counts, weights_out=fresh)
+    ctx.check()
+    for b, n in ((0, length), (2, length - 5)):
+        assert torch.equal(place[b], before[b])
+        assert torch.equal(other[b, :, :n], before[b, :, :n]) and torch.all(other[b, :, n:] == 7.0)
+        assert torch.all(fresh[b, :, :n] == 0.0) and torch.all(fresh[b, :, n:] == 7.0)
+    assert torch.equal(place[1], torch.where(torch.arange(length, device=ctx.device) < 77, other[1], before[1]))
+
+
 @pytest.mark.parametrize("tokens", [1, 7, 90])
 def test_attention_queries_of_all_magnitudes(ctx, tokens):
     """Neighbouring queries that differ by up to 2^20, and rows of zeros."""
