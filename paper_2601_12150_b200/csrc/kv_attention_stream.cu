@@ -101,13 +101,15 @@ struct Share {
   int working, per, more;
   __device__ __forceinline__ Share(int total, int workers) {
     working = min(total, workers);
-    per = working ? total / working : 0;
-    more = working ? total % working : 0;
+    per = working ? (unsigned)total / (unsigned)working : 0;
+    more = total - per * working;
   }
   __device__ __forceinline__ int begin(int worker) const { return worker * per + min(worker, more); }
   __device__ __forceinline__ int owner(int t) const {
     const int wide = more * (per + 1);
-    return t < wide ? t / (per + 1) : more + (t - wide) / per;
+    const bool first = t < wide;
+    const unsigned q = (unsigned)(first ? t : t - wide) / (unsigned)(first ? per + 1 : per);
+    return first ? q : more + q;
   }
 };
 
@@ -170,8 +172,8 @@ __device__ __forceinline__ bool next_piece(const KvView& c, const KvAttnArgs& a,
   }
   const int off = w.pos - w.before;
   p.b = w.b;
-  p.head = off / tiles;
-  p.kt0 = off % tiles;
+  p.head = (unsigned)off / (unsigned)tiles;
+  p.kt0 = off - p.head * tiles;
   p.kt1 = min(tiles, p.kt0 + (w.end - w.pos));
   p.tiles = tiles;
   p.len = seq_len(c, w.b);
@@ -791,7 +793,7 @@ __global__ void __launch_bounds__(Layout<D, NT>::kThreads, 1)
 constexpr int kFinishThreads = 256;
 
 __device__ __forceinline__ const float2* part_ml(const StreamArgs& s, int workers, int row, int worker, int c0) {
-  return s.part_ml + (size_t)(2 * row + (worker == c0)) * workers + worker;
+  return s.part_ml + (unsigned)((2 * row + (worker == c0)) * workers + worker);
 }
 // Maximum and sum of `x` over `lanes` neighbouring threads; with it, what the caller's other sums are to be scaled by.
 __device__ __forceinline__ float2 join_lanes(float top, float den, int lanes, float* scale) {
@@ -871,13 +873,15 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
       if (c0 == c1) continue;
       // the blocks that meet the pair share its columns (four values of a row), and as many threads as there are share
       // a column's pieces; each finds the row's maximum and sum among them by itself, so that nothing waits for them
-      const int f0 = c0 / per_block, f1 = c1 / per_block, mine = blockIdx.x - f0;
-      const int columns = rows * (D / 4);
-      const int x0 = columns * mine / (f1 - f0 + 1), x1 = columns * (mine + 1) / (f1 - f0 + 1);
-      const int lanes = x1 - x0 >= joiners ? 1 : min(32, 1 << (31 - __clz(joiners / max(1, x1 - x0))));
+      // (the arithmetic around the loads is half of the second kernel's instructions: one unsigned division where it can be)
+      const unsigned f0 = (unsigned)c0 / (unsigned)per_block, f1 = (unsigned)c1 / (unsigned)per_block;
+      const unsigned columns = rows * (D / 4), width = (columns + f1 - f0) / (f1 - f0 + 1);
+      const int x0 = (blockIdx.x - f0) * width, x1 = min(columns, x0 + width);
+      // as many lanes a column, a power of two, as leave every column some: log2(joiners) less width's, rounded up
+      const int llanes = max(0, min(5, 31 - __clz(joiners) - (32 - __clz((int)width - 1)))), lanes = 1 << llanes;
       const int sub = threadIdx.x & (lanes - 1);
-      for (int xb = x0; xb < x1; xb += joiners / lanes) {
-        const int x = xb + (int)threadIdx.x / lanes;
+      for (int xb = x0; xb < x1; xb += joiners >> llanes) {
+        const int x = xb + (int)(threadIdx.x >> llanes);
         const int row = x / (D / 4), d = x % (D / 4) * 4;
         float top = -INFINITY, den = 0.0f, f;
         float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -891,7 +895,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
             v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (y <= c1) {
               ml[j] = *part_ml(s, workers, row, y, c0);
-              v[j] = *reinterpret_cast<const float4*>(s.part_o + ((size_t)(2 * y + (y == c0)) * row_slots + row) * D + d);
+              v[j] = *reinterpret_cast<const float4*>(s.part_o + (unsigned)(((2 * y + (y == c0)) * row_slots + row) * D + d));
             }
           }
           const float m = fmaxf(top, fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)));
@@ -919,7 +923,7 @@ __global__ void __launch_bounds__(kFinishThreads, 4)
           sum.w += __shfl_xor_sync(0xffffffffu, sum.w, o);
         }
         if (x < x1 && sub == 0) {
-          const int i = row / s.a.group, h = p.head * s.a.group + row % s.a.group;
+          const int i = (unsigned)row / (unsigned)s.a.group, h = p.head * s.a.group + row - i * s.a.group;
           f = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;                   // (a NaN stays one)
           uint2 u;
           if (s.a.dtype == SPV_BF16) u = make_uint2(kv_pack2<SPV_BF16>(sum.x * f, sum.y * f), kv_pack2<SPV_BF16>(sum.z * f, sum.w * f));
@@ -1020,8 +1024,8 @@ int32_t spv_kv_stream_run(spv_ctx* ctx, const spv_kv_cache* cache, const spv_kv_
   const int slots = row_slots_of(s.rows);
   // One pair a CTA, or the line and its second kernel?  A wave of CTAs costs the tiles of a warp and about two more; the
   // line costs its tiles, each about twice (the finishing kernel), and a fixed four.  Measured in us, alone against the line,
-  // equal lengths: 16 pairs of 785 slots of 64: 8.5, 12.9; 128 of 1536: 10.0, 19.4; 128 of 3000 slots of 128: 23, 35; 512 of
-  // 380: 25, 34; but 8 pairs of 2200: 17.5, 15.1; 512 of 100: 22, 20; 4096 of 50 slots of 64: 146, 40.  The bound of twelve
+  // equal lengths: 16 pairs of 785 slots of 64: 8.5, 12.7; 128 of 1536: 9.8, 18.7; 128 of 3000 slots of 128: 23, 35; 512 of
+  // 380: 25, 32; but 8 pairs of 2200: 17.8, 15.0; 512 of 100: 22, 20; 4096 of 50 slots of 64: 146, 42.  The bound of twelve
   // keeps one long pair among short ones from holding up the call.
   const int64_t pairs = (int64_t)seqs->batch * cache->kv_heads;
   const int64_t waves = (pairs + ctas - 1) / ctas, warps = warps_of(slots);
