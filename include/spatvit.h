@@ -296,6 +296,8 @@ typedef struct {
   const int32_t* page_table;         /* device [batch, columns]                                  */
   const int32_t* lengths;            /* device [batch]: tokens held, see each entry point        */
   int32_t max_length;                /* no length is larger; 0 => columns * block                */
+                                     /* (a close bound saves workspace, and a launch where few     */
+                                     /* or short sequences are read)                               */
 } spv_kv_seqs;
 
 /* Append up to `tokens` new tokens to every sequence.  seqs->lengths: tokens held BEFORE the call

@@ -535,7 +535,7 @@ class Context:
         written).  lse: optional fp32 [B, tokens, heads] to fill.  weights_out: optional fp32 [B, kv_heads, slots]:
         weights_in (default 0; may be weights_out itself) plus the attention weight that every kept token received.
         max_length: no sequence is longer (default: what the table and the weights have room for; the workspace grows
-        with it).  Returns out."""
+        with it, and few or short sequences take one launch less when it is close).  Returns out."""
         torch = self._torch
         dt = self._kv_dtype(q)
         shape = q.shape

@@ -362,6 +362,59 @@ def test_attention_where_the_pairs_become_many_or_long(ctx, sequences, tiles):
     run_attention(ctx, rng, lengths, 1, None, 2, 2, 64, 64, "int8", "fp16", True)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("columns", [12, 900])
+@pytest.mark.parametrize("tokens,group", [(1, 4), (3, 4), (2, 13)])
+def test_attention_of_odd_caches_in_narrow_and_wide_tables(ctx, fmt, columns, tokens, group):
+    """Scales many powers of two apart, a query that is not finite, and a page that is none: in a table that fits the
+    sequences, where a pair is a CTA's, and in one with room for far more, where pairs are lined up."""
+    import paper_2601_12150_b200 as spv
+    rng = np.random.default_rng(columns + group)
+    block, dim, heads = 16, 64, 2
+    lengths = [12 * block, 0, 5 * block - 3]
+    k, v = normals(rng, (3, lengths[0], heads, dim), "bf16", 0.3), normals(rng, (3, lengths[0], heads, dim), "bf16")
+    for i, e in enumerate([0, 12, -30, 0, 40, -60, 3, 0, -8, 20, 1, 0]):
+        v[:, i * block:(i + 1) * block] *= 2.0 ** e
+        k[:, i * block:(i + 1) * block] *= 2.0 ** -(i % 4)
+    v[0, 7 * block:8 * block] = 0
+    cache = make_cache(ctx, 20, heads, dim, block, fmt)
+    table, dtable = make_table(rng, lengths, block, 20, columns, ctx.device)
+    pool = ref.Pool(20, heads, block, dim, fmt)
+    dlen = torch.tensor(lengths, dtype=torch.int32, device=ctx.device)
+    ctx.kv_cache_append(cache, k.to(ctx.device), v.to(ctx.device), dtable, torch.zeros_like(dlen), counts=dlen)
+    for b, n in enumerate(lengths):
+        for h in range(heads):
+            for m, x in (("k", k), ("v", v)):
+                pool.append(m, table[b], 0, x[b, :n, h].double().numpy(), h)
+    state = (cache, pool, table, dtable, dlen)
+    for weights in (True, False):        # (without weights it is the table alone that says how long a sequence may be)
+        run_attention(ctx, rng, lengths, tokens, None, heads * group, heads, dim, block, fmt, "bf16", True, weights=weights,
+                      state=state)
+    q = normals(rng, (3, tokens, heads * group, dim), "bf16")
+    exact = [ref.attention(pool, table[b], q[b].double().numpy(), n, tokens, heads * group, heads, True, 0.125)
+             for b, n in enumerate(lengths)]
+    for value in (float("nan"), float("inf")):
+        bad = q.clone()
+        bad[0, tokens - 1, 1, 5] = value
+        got = ctx.kv_cache_attention(cache, bad.to(ctx.device), dtable, dlen).cpu().double().numpy()
+        ctx.check()
+        assert np.isnan(got[0, tokens - 1, 1]).all()
+        for b, (o, _, _, spread, reach, vmax) in enumerate(exact):
+            fine = np.abs(got[b] - o) <= bounds(o, spread, reach, vmax, dim, max(1, lengths[b]), "bf16")
+            if b == 0:
+                fine[tokens - 1, 1] = True
+            assert fine.all()
+    # a page that is none, of the last sequence: found, skipped, and the first sequence as it was
+    lost = dtable.clone()
+    lost[2, 1] = cache.pages
+    good = ctx.kv_cache_attention(cache, q.to(ctx.device), dtable, dlen)
+    got = ctx.kv_cache_attention(cache, q.to(ctx.device), lost, dlen)
+    with pytest.raises(spv.SpvError) as e:
+        ctx.check()
+    assert e.value.status == spv.ERR_INVALID_ARG
+    assert torch.equal(got[:2], good[:2]) and torch.isfinite(got).all()
+
+
 @pytest.mark.parametrize("length,room", [(300, 0), (300, 9000), (9000, 0)])
 @pytest.mark.parametrize("tokens", [1, 40])
 def test_attention_weights_of_sequences_that_ask_nothing(ctx, length, room, tokens):
